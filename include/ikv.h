@@ -42,7 +42,8 @@
  *    kernels do not check them (an id outside the pool reads or writes outside
  *    it). With IKV_DEBUG=1 in the environment (read on every call), the calls
  *    that read such ids (score_history, redirect_slots, decode_attend_slotmap,
- *    compact_apply, prefill_span) first copy them to the host, after the
+ *    compact_apply, prefill_span, quant_store, quant_load, decode_attend_quant,
+ *    attend_chunk, attend_chunk_quant) first copy them to the host, after the
  *    stream's earlier work, and return IKV_EINVAL naming the session, the array
  *    and the index of the first bad entry, with no kernel launched. This
  *    synchronises the stream on every call; it is meant for debugging.
@@ -69,6 +70,10 @@ typedef int32_t ikv_status;
 #define IKV_BF16 0
 #define IKV_F32  1
 
+/* Codes of the 8-bit cache (ikv_quant_pool). */
+#define IKV_INT8 0
+#define IKV_E4M3 1
+
 /* ikv_score_history flags. */
 #define IKV_RESIDUAL  1u   /* add alpha * MLP(phi ++ c), Eq. 4 (needs `residual`)           */
 #define IKV_NO_XATTN  2u   /* the "- x-attn" ablation: c_j = 0 in Eq. 4 (Sec. 3.3)          */
@@ -82,6 +87,7 @@ typedef int32_t ikv_status;
 #define IKV_CALL_DECODE   4
 #define IKV_CALL_COMPACT  5
 #define IKV_CALL_PREFILL  6
+#define IKV_CALL_CHUNK    7
 
 /*
  * The paged KV pool (Sec. 3.1: post-RoPE K, V in R^{L x Hkv x N x D}, stored by
@@ -418,6 +424,114 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
                             const int32_t *hist, const int32_t *n_hist, double rope_base,
                             float lambda, float *M, void *q_out, void *out, float *kq,
                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The 8-bit cache: K and V rows by physical slot like the pool, each row of one layer,
+ * slot and KV head as D one-byte codes and a float32 scale.
+ *   k_codes, v_codes: device, [L][num_slots][Hkv][D] bytes, 16-byte aligned.
+ *   scales: device float32, [L][num_slots][Hkv][2], 8-byte aligned: the scale of the K
+ *           row, then of the V row.
+ *   code: IKV_INT8 (two's complement, -127 .. 127) or IKV_E4M3 (OCP FP8 E4M3: 4 exponent
+ *         and 3 mantissa bits, largest 448).
+ *   io_dtype: IKV_BF16 or IKV_F32, the type of q and out in the attention calls.
+ *   dead_slot: as in ikv_pool; its row is neither written nor read.
+ * A row stands for code * scale. With a = max(max_d |x_d|, 2^-100) over the row:
+ *   IKV_INT8  scale = a / 127 (rounded to float32), code_d = 127 x_d / a rounded to the
+ *             nearest whole number, ties to even (of the quotient itself, not of a rounded
+ *             one: the code does not depend on the precision it is computed in);
+ *   IKV_E4M3  scale = the least power of two with 448 scale >= a, code_d = x_d / scale
+ *             rounded to the nearest E4M3 value, ties to even. A power of two costs a
+ *             floating code no precision, and makes reading back exact, in bf16 too.
+ * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
+ * every channel. L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
+ * of a larger cache is a descriptor with L = 1 and pointers to that layer.
+ */
+typedef struct ikv_quant_pool {
+  int32_t L, Hq, Hkv, D;
+  int64_t num_slots;
+  int32_t dead_slot;
+  int32_t code;
+  int32_t io_dtype;
+  int32_t reserved;            /* 0 */
+  void *k_codes;
+  void *v_codes;
+  float *scales;
+} ikv_quant_pool;
+
+/*
+ * Quantise rows of a pool into the 8-bit cache: for session b, k < min(n_rows[b], N) and
+ * every layer and KV head, the K and V rows at slot src[slot_off + k] of `pool` go to slot
+ * dst[slot_off + k] of `cache`. Uses: new tokens (a pool of the new rows, src NULL), the
+ * kept rows of a retention event (src = dst = the live list), a change of slots.
+ *   src: device int32 per session [N], or NULL: row slot_off + k of the pool.
+ *   dst: device int32 per session [N]; entries equal to cache->dead_slot are skipped (the
+ *        padding of a batch). A slot may be listed once only in a call; rows of slots that
+ *        are not listed stay as they are.
+ *   n_rows: device int32 [B], or NULL: N rows per session; values are clamped to [0, N].
+ * pool and cache must agree in L, Hkv and D (IKV_ESHAPE); the pool's rows are bf16 or
+ * float32, 16-byte aligned. Needs no workspace. Only N and slot_off of the sessions are read.
+ */
+ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool,
+                           const ikv_session *sess, const ikv_session *sess_dev, int32_t B,
+                           const int32_t *src, const int32_t *dst, const int32_t *n_rows,
+                           void *stream);
+
+/*
+ * Read rows of the 8-bit cache back into a pool: code * scale in float32, rounded to the
+ * pool's type (nearest even), from slot src[slot_off + k] of `cache` to slot
+ * dst[slot_off + k] of `pool` (dst NULL: row slot_off + k). Entries whose src is
+ * cache->dead_slot are skipped and leave the pool's row as it is. Otherwise as
+ * ikv_quant_store: a destination may be listed once only in a call.
+ */
+ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
+                          const ikv_session *sess, const ikv_session *sess_dev, int32_t B,
+                          const int32_t *src, const int32_t *dst, const int32_t *n_rows,
+                          void *stream);
+
+/*
+ * Attention over the 8-bit cache, and attention of a chunk of new tokens over a pool or
+ * the 8-bit cache.
+ *   live, n_live: the session's list of slots, oldest first, new tokens last (as
+ *     ikv_redirect_slots writes it, the slots of new tokens appended; n_live[b] is clamped
+ *     to [0, N]). The new tokens' rows are in the cache already.
+ *   The chunk is the list's newest n entries: n = 1 for ikv_decode_attend_quant, n = qe - qs
+ *     for the chunk calls. Token t of it has the list entry i = n_live - n + t and sees entry
+ *     j iff  j <= i  and  (window == 0  or  j < sinks  or  j > i - window): the newest
+ *     `window` entries up to its own, and the first `sinks`, which stay visible. Both count
+ *     entries of the list, so positions that a retention event dropped take no room in the
+ *     window. A token with i < 0 (a list shorter than its chunk) sees nothing and its output
+ *     is zero. sinks and window are >= 0; window 0 means none, and sinks is then ignored.
+ *   out = softmax_j(q . K_j / sqrt(D)) . V_j over the entries seen, softmax and sums in
+ *     float32. Entries a token does not see add nothing to it, whatever their rows hold.
+ *   q, out: device, 16-byte aligned, packed by session (session b's rows start after those of
+ *     the sessions before it), [L][Hq][n][D] each: [B][L][Hq][D] for the decode. Their type is
+ *     io_dtype of the cache, or bf16 for ikv_attend_chunk, which needs a bf16 pool
+ *     (IKV_EUNSUPPORTED otherwise). q and out may not overlap.
+ *   workspace: ikv_workspace_bytes / ikv_quant_workspace_bytes with IKV_CALL_DECODE or
+ *     IKV_CALL_CHUNK (the same for every sinks and window).
+ *   As with ikv_decode_attend_slotmap, long lists are split across workgroups by bounds known
+ *   on the host, min(N, max(C, pi + qe - qs)) entries for the decode and N for the chunk calls;
+ *   the order of the sums depends on them.
+ */
+ikv_status ikv_decode_attend_quant(const ikv_quant_pool *cache, const ikv_session *sess,
+                                   const ikv_session *sess_dev, int32_t B, const void *q,
+                                   const int32_t *live, const int32_t *n_live, int32_t sinks,
+                                   int32_t window, void *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+ikv_status ikv_attend_chunk(const ikv_pool *pool, const ikv_session *sess,
+                            const ikv_session *sess_dev, int32_t B, const void *q,
+                            const int32_t *live, const int32_t *n_live, int32_t sinks,
+                            int32_t window, void *out, void *workspace, size_t workspace_bytes,
+                            void *stream);
+ikv_status ikv_attend_chunk_quant(const ikv_quant_pool *cache, const ikv_session *sess,
+                                  const ikv_session *sess_dev, int32_t B, const void *q,
+                                  const int32_t *live, const int32_t *n_live, int32_t sinks,
+                                  int32_t window, void *out, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/* ikv_workspace_bytes for the calls on the 8-bit cache: IKV_CALL_DECODE or IKV_CALL_CHUNK. */
+ikv_status ikv_quant_workspace_bytes(const ikv_quant_pool *cache, const ikv_session *sess,
+                                     int32_t B, int32_t call, size_t *bytes);
 
 /*
  * Workspace size of one call (IKV_CALL_*) for these sessions, in bytes (0 when

@@ -74,6 +74,24 @@ ikv_status check_pool(const ikv_pool *p) {
   return IKV_OK;
 }
 
+ikv_status check_quant_pool(const ikv_quant_pool *c) {
+  if (!c) return fail(IKV_EINVAL, "cache is NULL");
+  if (c->L < 1 || c->Hq < 1 || c->Hkv < 1) return fail(IKV_ESHAPE, "cache: L, Hq, Hkv must be >= 1");
+  if (c->Hq % c->Hkv) return fail(IKV_ESHAPE, "cache: Hq (%d) is not a multiple of Hkv (%d)", c->Hq, c->Hkv);
+  if (c->Hq / c->Hkv > 8) return fail(IKV_EUNSUPPORTED, "cache: Hq/Hkv = %d > 8", c->Hq / c->Hkv);
+  if (c->D != 64 && c->D != 128) return fail(IKV_EUNSUPPORTED, "cache: D = %d (supported: 64, 128)", c->D);
+  if (c->num_slots < 1 || c->num_slots > INT32_MAX) return fail(IKV_ESHAPE, "cache: num_slots out of range");
+  if (c->dead_slot < 0 || c->dead_slot >= c->num_slots) return fail(IKV_ESHAPE, "cache: dead_slot out of range");
+  if (c->code != IKV_INT8 && c->code != IKV_E4M3) return fail(IKV_EINVAL, "cache: unknown code %d", c->code);
+  if (c->io_dtype != IKV_BF16 && c->io_dtype != IKV_F32) return fail(IKV_EINVAL, "cache: unknown io_dtype %d", c->io_dtype);
+  if (c->reserved != 0) return fail(IKV_EINVAL, "cache: reserved must be 0");
+  if (!c->k_codes || !c->v_codes || !c->scales) return fail(IKV_EINVAL, "cache: k_codes / v_codes / scales is NULL");
+  if ((reinterpret_cast<uintptr_t>(c->k_codes) | reinterpret_cast<uintptr_t>(c->v_codes)) % 16 ||
+      reinterpret_cast<uintptr_t>(c->scales) % 8)
+    return fail(IKV_EINVAL, "cache: k_codes and v_codes must be 16-byte aligned, scales 8-byte aligned");
+  return IKV_OK;
+}
+
 ikv_status check_sessions(const ikv_session *s, const ikv_session *sd, int32_t B) {
   if (B < 0) return fail(IKV_EINVAL, "B < 0");
   if (B > 0 && (!s || !sd)) return fail(IKV_EINVAL, "sess / sess_dev is NULL");
@@ -160,6 +178,32 @@ size_t prefill_bytes(const ikv_pool *p, const ikv_session *s, int B) {
                 ikv::prefill_part_floats(p->L, p->Hkv, B, prefill_splits(p, s, B), p->D)) * sizeof(float);
 }
 
+ikv::AttendArgs attend_args(const ikv_pool *p) {
+  ikv::AttendArgs a{};
+  a.L = p->L, a.Hq = p->Hq, a.Hkv = p->Hkv, a.D = p->D;
+  a.num_slots = p->num_slots;
+  a.format = ikv::KV_BF16;
+  a.io_f32 = false;
+  a.k = p->k_pool, a.v = p->v_pool, a.scales = nullptr;
+  return a;
+}
+
+ikv::AttendArgs attend_args(const ikv_quant_pool *c) {
+  ikv::AttendArgs a{};
+  a.L = c->L, a.Hq = c->Hq, a.Hkv = c->Hkv, a.D = c->D;
+  a.num_slots = c->num_slots;
+  a.format = c->code == IKV_INT8 ? ikv::KV_INT8 : ikv::KV_E4M3;
+  a.io_f32 = c->io_dtype == IKV_F32;
+  a.k = c->k_codes, a.v = c->v_codes, a.scales = c->scales;
+  return a;
+}
+
+// The workspace of an attention call, by its longest possible split (no window).
+size_t attend_bytes(ikv::AttendArgs a, const ikv_session *s, int B, bool decode) {
+  ikv::AttendPlan plan = ikv::attend_plan(a, s, B, decode, 0, 0);
+  return size_t(plan.ws_floats) * sizeof(float);
+}
+
 ikv_status pending_fault() {
   if (ikv::take_host_fault())
     return fail(IKV_EHIP, "a wait between workgroups of an earlier call (ikv_select_budget's grid barrier) gave up; "
@@ -206,10 +250,93 @@ ikv_status debug_count(const int32_t *counts, int b, int64_t cap, hipStream_t st
   return IKV_OK;
 }
 
+// The live lists of an attention call.
+ikv_status debug_live(const ikv_session *sess, int B, const int32_t *live, const int32_t *n_live, int64_t num_slots,
+                      hipStream_t st) {
+  for (int b = 0; b < B; ++b) {
+    int64_t nl = 0;
+    if (ikv_status r = debug_count(n_live, b, sess[b].N, st, "n_live", &nl)) return r;
+    if (ikv_status r = debug_ids(live, sess[b].slot_off, nl, 0, num_slots, st, "live", b)) return r;
+  }
+  return IKV_OK;
+}
+
+// The slot lists of a store into, or a load from, the 8-bit cache: ids in range, and no
+// destination listed twice among the entries that are not skipped.
+ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache_ids, int64_t cache_slots,
+                            const char *cache_what, int32_t dead, const int32_t *pool_ids, int64_t pool_slots,
+                            const char *pool_what, bool to_cache, const int32_t *n_rows, hipStream_t st) {
+  std::vector<int32_t> h, hp, written;
+  for (int b = 0; b < B; ++b) {
+    int64_t n = sess[b].N;
+    if (n_rows)
+      if (ikv_status r = debug_count(n_rows, b, n, st, "n_rows", &n)) return r;
+    if (ikv_status r = debug_ids(cache_ids, sess[b].slot_off, n, 0, cache_slots, st, cache_what, b)) return r;
+    if (pool_ids)
+      if (ikv_status r = debug_ids(pool_ids, sess[b].slot_off, n, 0, pool_slots, st, pool_what, b)) return r;
+    if (ikv_status r = debug_fetch(h, cache_ids + sess[b].slot_off, n, st, cache_what, b)) return r;
+    if (!to_cache && pool_ids)
+      if (ikv_status r = debug_fetch(hp, pool_ids + sess[b].slot_off, n, st, pool_what, b)) return r;
+    for (int64_t k = 0; k < n; ++k)
+      if (h[size_t(k)] != dead)
+        written.push_back(to_cache ? h[size_t(k)] : pool_ids ? hp[size_t(k)] : int32_t(sess[b].slot_off + k));
+  }
+  std::sort(written.begin(), written.end());
+  const auto twice = std::adjacent_find(written.begin(), written.end());
+  if (twice != written.end()) return fail(IKV_EINVAL, "IKV_DEBUG: destination slot %d is listed twice", *twice);
+  return IKV_OK;
+}
+
 ikv_status debug_slot_maps(const ikv_session *sess, int B, const int32_t *slot_maps, int64_t num_slots,
                            hipStream_t st) {
   for (int b = 0; b < B; ++b)
     if (ikv_status r = debug_ids(slot_maps, sess[b].slot_off, sess[b].N, 0, num_slots, st, "slot map", b)) return r;
+  return IKV_OK;
+}
+
+// The checks and the launch that the attention calls of this kind share.
+ikv_status attend(ikv::AttendArgs a, const ikv_session *sess, const ikv_session *sess_dev, int32_t B, bool decode,
+                  const void *q, const int32_t *live, const int32_t *n_live, int32_t sinks, int32_t window, void *out,
+                  void *workspace, size_t workspace_bytes, void *stream, const char *what) {
+  ikv_status r;
+  if ((r = check_sessions(sess, sess_dev, B))) return r;
+  if (sinks < 0 || window < 0) return fail(IKV_EINVAL, "sinks and window must be >= 0 (got %d, %d)", sinks, window);
+  if (B == 0) return ok();
+  if (!q || !live || !n_live || !out) return fail(IKV_EINVAL, "q / live / n_live / out is NULL");
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) % 16)
+    return fail(IKV_EINVAL, "q and out must be 16-byte aligned");
+  if ((r = check_ws(workspace, workspace_bytes, attend_bytes(a, sess, B, decode)))) return r;
+  const ikv::AttendPlan plan = ikv::attend_plan(a, sess, B, decode, sinks, window);
+  if (plan.max_n == 0) return ok();
+  if (plan.too_large) return fail(IKV_EUNSUPPORTED, "%s: too many sessions, layers and query rows for one launch", what);
+  if (debug_mode() && (r = debug_live(sess, B, live, n_live, a.num_slots, (hipStream_t)stream))) return r;
+  a.sess = sess_dev, a.B = B, a.decode = decode;
+  a.q = q, a.live = live, a.n_live = n_live, a.out = out;
+  a.sinks = window ? sinks : 0, a.window = window;
+  a.ws = static_cast<float *>(workspace);
+  return hip_status(ikv::launch_attend(a, plan, (hipStream_t)stream), what);
+}
+
+// The checks that the store into and the load from the 8-bit cache share.
+ikv_status check_quant_rows(const ikv_quant_pool *c, const ikv_pool *p, const ikv_session *sess,
+                            const ikv_session *sess_dev, int32_t B, const int32_t *cache_ids, const char *cache_what,
+                            const int32_t *pool_ids) {
+  ikv_status r;
+  if ((r = check_quant_pool(c))) return r;
+  if ((r = check_pool(p))) return r;
+  if (c->L != p->L || c->Hkv != p->Hkv || c->D != p->D)
+    return fail(IKV_ESHAPE, "cache and pool differ in L, Hkv or D (%d, %d, %d and %d, %d, %d)", c->L, c->Hkv, c->D, p->L,
+                p->Hkv, p->D);
+  if ((reinterpret_cast<uintptr_t>(p->k_pool) | reinterpret_cast<uintptr_t>(p->v_pool)) % 16)
+    return fail(IKV_EINVAL, "pool: k_pool and v_pool must be 16-byte aligned");
+  if ((r = check_sessions(sess, sess_dev, B))) return r;
+  if (B > 65535) return fail(IKV_EUNSUPPORTED, "B = %d > 65535", B);
+  if (B > 0 && !cache_ids) return fail(IKV_EINVAL, "%s is NULL", cache_what);
+  if (!pool_ids)
+    for (int b = 0; b < B; ++b)
+      if (sess[b].slot_off + sess[b].N > p->num_slots)
+        return fail(IKV_ESHAPE, "session %d: rows %lld .. %lld of a pool of %lld slots", b, (long long)sess[b].slot_off,
+                    (long long)(sess[b].slot_off + sess[b].N), (long long)p->num_slots);
   return IKV_OK;
 }
 
@@ -349,6 +476,11 @@ ikv_status ikv_workspace_bytes(const ikv_pool *pool, const ikv_session *sess, in
       if ((r = check_pool(pool))) return r;
       if ((r = check_sessions(sess, sess, B))) return r;
       *bytes = prefill_bytes(pool, sess, B);
+      return ok();
+    case IKV_CALL_CHUNK:
+      if ((r = check_pool(pool))) return r;
+      if ((r = check_sessions(sess, sess, B))) return r;
+      *bytes = attend_bytes(attend_args(pool), sess, B, false);
       return ok();
     case IKV_CALL_COMPACT:
       if ((r = check_sessions(sess, sess, B))) return r;
@@ -605,6 +737,78 @@ ikv_status ikv_decode_attend_slotmap(const ikv_pool *pool, const ikv_session *se
   return hip_status(ikv::launch_decode(*pool, sess_dev, B, splits, q, live, n_live, out,
                                        static_cast<float *>(workspace), (hipStream_t)stream),
                     "ikv_decode_attend_slotmap");
+}
+
+ikv_status ikv_quant_workspace_bytes(const ikv_quant_pool *cache, const ikv_session *sess, int32_t B, int32_t call,
+                                     size_t *bytes) {
+  if (!bytes) return fail(IKV_EINVAL, "bytes is NULL");
+  *bytes = 0;
+  ikv_status r;
+  if ((r = check_quant_pool(cache))) return r;
+  if ((r = check_sessions(sess, sess, B))) return r;
+  if (call != IKV_CALL_DECODE && call != IKV_CALL_CHUNK) return fail(IKV_EINVAL, "unknown call id %d", call);
+  *bytes = attend_bytes(attend_args(cache), sess, B, call == IKV_CALL_DECODE);
+  return ok();
+}
+
+ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool, const ikv_session *sess,
+                           const ikv_session *sess_dev, int32_t B, const int32_t *src, const int32_t *dst,
+                           const int32_t *n_rows, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  ikv_status r = check_quant_rows(cache, pool, sess, sess_dev, B, dst, "dst", src);
+  if (r) return r;
+  const int maxN = max_n(sess, B);
+  if (maxN == 0) return ok();
+  if (debug_mode() && (r = debug_quant_rows(sess, B, dst, cache->num_slots, "dst", cache->dead_slot, src,
+                                            pool->num_slots, "src", true, n_rows, (hipStream_t)stream)))
+    return r;
+  return hip_status(ikv::launch_quant_store(*cache, *pool, sess_dev, B, maxN, src, dst, n_rows, (hipStream_t)stream),
+                    "ikv_quant_store");
+}
+
+ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool, const ikv_session *sess,
+                          const ikv_session *sess_dev, int32_t B, const int32_t *src, const int32_t *dst,
+                          const int32_t *n_rows, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  ikv_status r = check_quant_rows(cache, pool, sess, sess_dev, B, src, "src", dst);
+  if (r) return r;
+  const int maxN = max_n(sess, B);
+  if (maxN == 0) return ok();
+  if (debug_mode() && (r = debug_quant_rows(sess, B, src, cache->num_slots, "src", cache->dead_slot, dst,
+                                            pool->num_slots, "dst", false, n_rows, (hipStream_t)stream)))
+    return r;
+  return hip_status(ikv::launch_quant_load(*cache, *pool, sess_dev, B, maxN, src, dst, n_rows, (hipStream_t)stream),
+                    "ikv_quant_load");
+}
+
+ikv_status ikv_decode_attend_quant(const ikv_quant_pool *cache, const ikv_session *sess, const ikv_session *sess_dev,
+                                   int32_t B, const void *q, const int32_t *live, const int32_t *n_live, int32_t sinks,
+                                   int32_t window, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  if (ikv_status r = check_quant_pool(cache)) return r;
+  return attend(attend_args(cache), sess, sess_dev, B, true, q, live, n_live, sinks, window, out, workspace,
+                workspace_bytes, stream, "ikv_decode_attend_quant");
+}
+
+ikv_status ikv_attend_chunk(const ikv_pool *pool, const ikv_session *sess, const ikv_session *sess_dev, int32_t B,
+                            const void *q, const int32_t *live, const int32_t *n_live, int32_t sinks, int32_t window,
+                            void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  if (ikv_status r = check_pool(pool)) return r;
+  if (pool->kv_dtype != IKV_BF16) return fail(IKV_EUNSUPPORTED, "ikv_attend_chunk needs a bf16 pool");
+  if ((reinterpret_cast<uintptr_t>(pool->k_pool) | reinterpret_cast<uintptr_t>(pool->v_pool)) % 16)
+    return fail(IKV_EINVAL, "pool: k_pool and v_pool must be 16-byte aligned");
+  return attend(attend_args(pool), sess, sess_dev, B, false, q, live, n_live, sinks, window, out, workspace,
+                workspace_bytes, stream, "ikv_attend_chunk");
+}
+
+ikv_status ikv_attend_chunk_quant(const ikv_quant_pool *cache, const ikv_session *sess, const ikv_session *sess_dev,
+                                  int32_t B, const void *q, const int32_t *live, const int32_t *n_live, int32_t sinks,
+                                  int32_t window, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  if (ikv_status r = check_quant_pool(cache)) return r;
+  return attend(attend_args(cache), sess, sess_dev, B, false, q, live, n_live, sinks, window, out, workspace,
+                workspace_bytes, stream, "ikv_attend_chunk_quant");
 }
 
 }  // extern "C"

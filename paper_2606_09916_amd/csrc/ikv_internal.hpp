@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "attend.hpp"
 #include "decode_plan.hpp"
 #include "ikv.h"
 #include "ikv_error.hpp"
@@ -321,6 +322,11 @@ hipError_t launch_prefill(const ikv_pool &pool, const ikv_session *sess_dev, int
                           const int32_t *hist, const int32_t *n_hist, double base, float decay, float *M,
                           void *q_out, void *out, float *kq, float *ws, int64_t kq_floats, hipStream_t st);
 
+hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+                              const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
+hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+                             const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 
 // A word of pinned host memory that kernels set (system scope) to report a fault the
 // host cannot see otherwise (a grid barrier that gave up). Allocated on first use and

@@ -14,8 +14,9 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libikv.so")
 
 IKV_BF16, IKV_F32 = 0, 1
+IKV_INT8, IKV_E4M3 = 0, 1
 IKV_RESIDUAL, IKV_NO_XATTN, IKV_POOL7, IKV_TWO_PASS = 1, 2, 4, 8
-CALL_SCORE, CALL_SELECT, CALL_REDIRECT, CALL_DECODE, CALL_COMPACT, CALL_PREFILL = 1, 2, 3, 4, 5, 6
+CALL_SCORE, CALL_SELECT, CALL_REDIRECT, CALL_DECODE, CALL_COMPACT, CALL_PREFILL, CALL_CHUNK = 1, 2, 3, 4, 5, 6, 7
 STATUS = {0: "IKV_OK", -1: "IKV_EINVAL", -2: "IKV_ESHAPE", -3: "IKV_EWORKSPACE", -4: "IKV_EUNSUPPORTED",
           -5: "IKV_EHIP"}
 
@@ -24,7 +25,8 @@ SYMBOLS = ("ikv_init_dead_slot", "ikv_qm_update", "ikv_score_history", "ikv_sele
            "ikv_redirect_slots", "ikv_decode_attend_slotmap", "ikv_workspace_bytes", "ikv_last_error",
            "ikv_timing", "ikv_timing_read", "ikv_memstore_create", "ikv_memstore_destroy", "ikv_memstore_acquire",
            "ikv_memstore_release", "ikv_memstore_trigger", "ikv_memstore_size", "ikv_resolve_span",
-           "ikv_compact_apply", "ikv_prefill_span")
+           "ikv_compact_apply", "ikv_prefill_span", "ikv_quant_store", "ikv_quant_load", "ikv_decode_attend_quant",
+           "ikv_attend_chunk", "ikv_attend_chunk_quant", "ikv_quant_workspace_bytes")
 IKV_KEY_EXPLICIT, IKV_KEY_SPAN, IKV_KEY_PREFIX, IKV_KEY_LOCAL = 1, 2, 3, 4
 
 
@@ -38,6 +40,12 @@ class Pool(ctypes.Structure):
     _fields_ = [("L", c_int32), ("Hq", c_int32), ("Hkv", c_int32), ("D", c_int32),
                 ("num_slots", c_int64), ("dead_slot", c_int32), ("kv_dtype", c_int32),
                 ("k_pool", c_void_p), ("v_pool", c_void_p)]
+
+
+class QuantPool(ctypes.Structure):
+    _fields_ = [("L", c_int32), ("Hq", c_int32), ("Hkv", c_int32), ("D", c_int32),
+                ("num_slots", c_int64), ("dead_slot", c_int32), ("code", c_int32), ("io_dtype", c_int32),
+                ("reserved", c_int32), ("k_codes", c_void_p), ("v_codes", c_void_p), ("scales", c_void_p)]
 
 
 class Session(ctypes.Structure):
@@ -61,7 +69,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2606_09916_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        P, S = ctypes.POINTER(Pool), ctypes.POINTER(Session)
+        P, S, Q = ctypes.POINTER(Pool), ctypes.POINTER(Session), ctypes.POINTER(QuantPool)
         sig = {
             "ikv_init_dead_slot": [P, c_void_p],
             "ikv_qm_update": [P, S, c_void_p, c_int32, c_void_p, c_void_p, c_float, c_void_p],
@@ -81,6 +89,15 @@ def lib() -> ctypes.CDLL:
             "ikv_prefill_span": [P, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                  ctypes.c_double, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
                                  c_void_p],
+            "ikv_quant_store": [Q, P, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p],
+            "ikv_quant_load": [Q, P, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p],
+            "ikv_decode_attend_quant": [Q, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                        c_void_p, c_void_p, c_size_t, c_void_p],
+            "ikv_attend_chunk": [P, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                                 c_void_p, c_size_t, c_void_p],
+            "ikv_attend_chunk_quant": [Q, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                       c_void_p, c_void_p, c_size_t, c_void_p],
+            "ikv_quant_workspace_bytes": [Q, S, c_int32, c_int32, ctypes.POINTER(c_size_t)],
             "ikv_timing": [c_int32],
             "ikv_memstore_create": [c_int32, ctypes.POINTER(c_void_p)],
             "ikv_memstore_acquire": [c_void_p, ctypes.POINTER(KeySource), ctypes.POINTER(c_int32),
@@ -119,6 +136,29 @@ def _stream(stream) -> int | None:
     return s.cuda_stream
 
 
+def _need(ok, status: int, func: str, msg: str) -> None:
+    if not ok:
+        raise IkvError(status, func, msg)
+
+
+def _tensor(t, dtype, numel: int, func: str, name: str) -> None:
+    """A tensor argument as the kernels read it: this type, whole rows in order, at least this many elements."""
+    _need(t.dtype == dtype, -1, func, f"{name} is {t.dtype}, not {dtype}")
+    _need(t.is_contiguous(), -1, func, f"{name} is not contiguous")
+    _need(t.numel() >= numel, -2, func, f"{name} has {t.numel()} elements, {numel} needed")
+
+
+def _place(func: str, sess, stream, *tensors) -> None:
+    """Every tensor on the device of the stream that the call is enqueued on."""
+    import torch
+    dev = sess.dev.device
+    for t in tensors:
+        _need(t is None or t.device == dev, -1, func, "tensors and sessions on different devices")
+    _need(dev.type == "cuda", -1, func, f"sessions are on {dev}, not on a GPU")
+    on = stream.device.index if stream is not None else torch.cuda.current_device()
+    _need(dev.index == on, -1, func, f"tensors are on {dev}, the stream is on cuda:{on}")
+
+
 # ----------------------------------------------------------------------------- descriptors
 
 def make_pool(k_pool, v_pool, L, Hq, Hkv, D, num_slots, dead_slot=0) -> Pool:
@@ -126,6 +166,24 @@ def make_pool(k_pool, v_pool, L, Hq, Hkv, D, num_slots, dead_slot=0) -> Pool:
     import torch
     dt = {torch.bfloat16: IKV_BF16, torch.float32: IKV_F32}[k_pool.dtype]
     return Pool(L, Hq, Hkv, D, num_slots, dead_slot, dt, k_pool.data_ptr(), v_pool.data_ptr())
+
+
+def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slot=0, io_dtype=None) -> QuantPool:
+    """8-bit cache descriptor over device tensors: codes [L][num_slots][Hkv][D] (int8 or float8_e4m3fn), scales
+    [L][num_slots][Hkv][2] float32 (K's, V's). io_dtype: q and out of the attention calls, bfloat16 (the default) or
+    float32."""
+    import torch
+    code = {torch.int8: IKV_INT8, torch.float8_e4m3fn: IKV_E4M3}.get(k_codes.dtype)
+    io = {None: IKV_BF16, torch.bfloat16: IKV_BF16, torch.float32: IKV_F32}.get(io_dtype)
+    what = "make_quant_pool"
+    _need(code is not None, -1, what, f"codes of type {k_codes.dtype} (int8 or float8_e4m3fn)")
+    _need(io is not None, -1, what, f"io_dtype {io_dtype} (bfloat16 or float32)")
+    rows = L * num_slots * Hkv
+    _tensor(k_codes, k_codes.dtype, rows * D, what, "k_codes")
+    _tensor(v_codes, k_codes.dtype, rows * D, what, "v_codes")
+    _tensor(scales, torch.float32, rows * 2, what, "scales")
+    return QuantPool(L, Hq, Hkv, D, num_slots, dead_slot, code, io, 0, k_codes.data_ptr(), v_codes.data_ptr(),
+                     scales.data_ptr())
 
 
 class Sessions:
@@ -247,6 +305,81 @@ def prefill_span(pool: Pool, sess: Sessions, slot_maps, q_raw, k_raw, v_raw, his
                                   _ptr(q_raw), _ptr(k_raw), _ptr(v_raw), _ptr(hist), _ptr(n_hist), float(rope_base),
                                   float(lam), _ptr(M), _ptr(q_out), _ptr(out), _ptr(kq), wp, wn, _stream(stream)),
            "ikv_prefill_span")
+
+
+def quant_workspace_bytes(cache: QuantPool, sess: Sessions, call: int) -> int:
+    n = c_size_t(0)
+    _check(lib().ikv_quant_workspace_bytes(ctypes.byref(cache), sess.host_ptr, sess.B, call, ctypes.byref(n)),
+           "ikv_quant_workspace_bytes")
+    return n.value
+
+
+def _lists(sess: Sessions, ids, counts, func: str, names) -> None:
+    """The per-entry slot lists (None where the call allows it) and the per-session counts."""
+    import torch
+    total = max((sess.host[b].slot_off + sess.host[b].N for b in range(sess.B)), default=0)
+    for t, name in zip(ids, names):
+        if t is not None:
+            _tensor(t, torch.int32, total, func, name)
+    if counts is not None:
+        _tensor(counts, torch.int32, sess.B, func, "the counts")
+
+
+def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=None, stream=None) -> None:
+    """Quantise rows of a pool into the 8-bit cache: slot src[k] (None: row slot_off + k) of the pool to slot dst[k]."""
+    _lists(sess, (src, dst), n_rows, "ikv_quant_store", ("src", "dst"))
+    _place("ikv_quant_store", sess, stream, src, dst, n_rows)
+    _check(lib().ikv_quant_store(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
+                                 _ptr(dst), _ptr(n_rows), _stream(stream)), "ikv_quant_store")
+
+
+def quant_load(cache: QuantPool, pool: Pool, sess: Sessions, src, dst=None, n_rows=None, stream=None) -> None:
+    """Read rows of the 8-bit cache back: slot src[k] of the cache to slot dst[k] (None: row slot_off + k) of the pool."""
+    _lists(sess, (src, dst), n_rows, "ikv_quant_load", ("src", "dst"))
+    _place("ikv_quant_load", sess, stream, src, dst, n_rows)
+    _check(lib().ikv_quant_load(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
+                                _ptr(dst), _ptr(n_rows), _stream(stream)), "ikv_quant_load")
+
+
+def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sinks: int, window: int, tokens: int, io,
+            stream) -> None:
+    import torch
+    numel = tokens * cache.L * cache.Hq * cache.D
+    dt = torch.float32 if io == IKV_F32 else torch.bfloat16
+    _tensor(q, dt, numel, func, "q")
+    _tensor(out, dt, numel, func, "out")
+    _lists(sess, (live,), n_live, func, ("live",))
+    _place(func, sess, stream, q, out, live, n_live)
+    _check(getattr(lib(), func)(ctypes.byref(cache), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(q), _ptr(live),
+                                _ptr(n_live), sinks, window, _ptr(out), wp, wn, _stream(stream)), func)
+
+
+def _chunk_tokens(sess: Sessions) -> int:
+    return sum(sess.host[b].qe - sess.host[b].qs for b in range(sess.B))
+
+
+def decode_attend_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
+                        window: int = 0, stream=None) -> None:
+    """One new token per session over the 8-bit cache: q, out [B][L][Hq][D] of the cache's io_dtype."""
+    wp, wn = ws.get(quant_workspace_bytes(cache, sess, CALL_DECODE))
+    _attend("ikv_decode_attend_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, sess.B, cache.io_dtype,
+            stream)
+
+
+def attend_chunk(pool: Pool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0, window: int = 0,
+                 stream=None) -> None:
+    """The newest qe - qs tokens of each session over a bf16 pool: q, out packed by session, [L][Hq][n][D]."""
+    wp, wn = ws.get(workspace_bytes(pool, sess, CALL_CHUNK))
+    _attend("ikv_attend_chunk", pool, sess, q, live, n_live, out, wp, wn, sinks, window, _chunk_tokens(sess), IKV_BF16,
+            stream)
+
+
+def attend_chunk_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
+                       window: int = 0, stream=None) -> None:
+    """attend_chunk over the 8-bit cache: q, out of the cache's io_dtype."""
+    wp, wn = ws.get(quant_workspace_bytes(cache, sess, CALL_CHUNK))
+    _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, _chunk_tokens(sess),
+            cache.io_dtype, stream)
 
 
 # ----------------------------------------------------------------------------- timing
