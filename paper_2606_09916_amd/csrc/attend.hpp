@@ -1,5 +1,5 @@
 // Arguments and launch plan of the attention over the 8-bit cache and of the chunk
-// attention (k_attend.hip). Plain C++: no HIP in here.
+// attention (k_attend*.hip). Plain C++: no HIP in here.
 #pragma once
 
 #include <stdint.h>
@@ -31,19 +31,49 @@ struct AttendArgs {
   float *ws;
 };
 
+constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all
+constexpr int FEW_ROUND = 1024;     // workgroups of one resident round of k_attend_few
+
 struct AttendPlan {
   int max_n;               // longest chunk of the batch
   bool too_large;          // does not fit a launch grid
+  bool few;                // every session's rows per KV head fit one 16-row block
+  int heads;               // adjacent KV heads of a workgroup (few)
+  int splits;              // of the entries of a session
+  int rows;                // rows per (session, layer, KV head) in the split state
   int64_t ws_floats;
 };
 
 inline int attend_tokens(const ikv_session &s, bool decode) { return decode ? 1 : std::max(0, s.qe - s.qs); }
 
+// Entries that a session's list may hold, as far as the host knows.
+inline int64_t attend_bound(const ikv_session &s, bool decode) {
+  return decode ? decode_live_bound(s) : std::max<int64_t>(1, s.N);
+}
+
 inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int B, bool decode, int sinks, int window) {
   AttendPlan p{};
-  for (int b = 0; b < B; ++b) p.max_n = std::max(p.max_n, attend_tokens(sess[b], decode));
+  const int G = a.Hq / a.Hkv;
+  int64_t longest = 1;
+  for (int b = 0; b < B; ++b) {
+    const int n = attend_tokens(sess[b], decode);
+    p.max_n = std::max(p.max_n, n);
+    int64_t len = attend_bound(sess[b], decode);
+    if (window) len = std::min<int64_t>(len, int64_t(sinks) + window + n);
+    longest = std::max(longest, len);
+  }
+  p.few = int64_t(p.max_n) * G <= FEW_ROWS;
+  p.splits = 1;
+  if (p.few) {
+    p.rows = p.max_n * G;
+    p.heads = a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1;
+    const int64_t wgs = std::max<int64_t>(1, int64_t(a.L) * (a.Hkv / p.heads) * std::max(1, B));
+    int64_t s = std::max<int64_t>(1, FEW_ROUND / wgs);
+    s = std::min<int64_t>(s, (longest + 127) / 128);
+    p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
+    if (p.splits > 1) p.ws_floats = int64_t(B) * a.L * a.Hkv * p.splits * p.rows * (a.D + 2);
+  }
   p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535;
-  p.ws_floats = 0;
   return p;
 }
 

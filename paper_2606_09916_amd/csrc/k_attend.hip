@@ -86,6 +86,7 @@ static void launch_attend_d(const AttendArgs &a, const AttendPlan &p, hipStream_
 }
 
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if (p.few) return launch_attend_few(a, p, st);
   if (a.format == KV_BF16) launch_attend_d<KV_BF16, uint16_t>(a, p, st);
   else if (a.format == KV_INT8) a.io_f32 ? launch_attend_d<KV_INT8, float>(a, p, st) : launch_attend_d<KV_INT8, uint16_t>(a, p, st);
   else a.io_f32 ? launch_attend_d<KV_E4M3, float>(a, p, st) : launch_attend_d<KV_E4M3, uint16_t>(a, p, st);

@@ -1,0 +1,401 @@
+// Attention of few query rows: the decode of one token, or a chunk of a few tokens whose
+// rows (n tokens x Hq / Hkv heads) of a KV head fit one 16-row matrix block.
+//
+// Bound by reading the rows of the list once (2 D + 8 bytes per entry, head and layer in
+// 8-bit form, 4 D in bf16). A wave owns one KV head and a split of the list and keeps
+// everything in registers; the waves of a workgroup own adjacent heads, so together they
+// read whole pieces of 4 rows. It walks blocks of 32 entries, the next block's rows on
+// their way while one is computed:
+//   S^T = K Q^T  (16 entries x 16 rows per product); lane (g, c) then holds entries
+//                16 kb + 4 g + i of row c, times their scales
+//   softmax      a reference per row and the sum of this lane's own weights; the reference
+//                moves only when a logit is FEW_SLACK above it (weights stay below 2^8)
+//   O^T += V^T P^T over the 32 entries. The contraction may take the entries in any order,
+//                so index 8 g + e stands for entry 4 g + e (e < 4) or 16 + 4 g + e - 4: the
+//                weights a lane holds are its operand as they are. A lane loads its D / 16
+//                channels of those 8 entries' value rows, and byte permutes make the
+//                operand of channel D / 16 c + j from them: no transpose through LDS.
+// Codes enter the products as bf16, exactly; scales multiply the logits and the weights in
+// float32. The weights are split into bf16 parts (two for bf16 outputs: 2^-17; three for
+// float32 ones, and three for float32 queries: 2^-25), which costs matrix work that the
+// reads hide.
+#include <math.h>
+
+#include <type_traits>
+
+#include "attend.hpp"
+#include "ikv_internal.hpp"
+#include "kv_codes.hpp"
+
+namespace ikv {
+
+constexpr float FEW_SLACK = 8.f;                 // log2
+constexpr int FEW_BLOCK = 32;                    // entries per block
+
+// x as bf16 parts, the first the nearest, each next one the nearest of what is left.
+template <int PARTS>
+__device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_k (&o)[PARTS]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float r = x[e];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      o[p][e] = __bf16(r);
+      r -= float(o[p][e]);
+    }
+  }
+}
+
+template <int FMT, typename IO, int D>
+__global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) {
+  constexpr int ES = FMT == KV_BF16 ? 2 : 1;     // bytes per element
+  constexpr int KS = D / 32;                     // 32-channel steps of the first product
+  constexpr int NC = D / 16;                     // channels of a lane in the second
+  constexpr int KW = D * ES / 64;                // 16-byte loads of a lane per 16 key rows
+  constexpr int VW = NC * ES / 4;                // words of a lane per value row
+  constexpr int QP = sizeof(IO) == 4 ? 3 : 1;    // bf16 parts of the queries
+  constexpr int PP = sizeof(IO) == 4 ? 3 : 2;    // and of the weights
+  __shared__ __align__(16) float sc[4][2][FEW_BLOCK];
+
+  const int b = blockIdx.z, heads = blockDim.x >> 6;
+  const ikv_session s = a.sess[b];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ngrp = a.Hkv / heads;
+  const int l = blockIdx.y / ngrp, hkv = (blockIdx.y - l * ngrp) * heads + w;
+  const int split = blockIdx.x, nsplit = gridDim.x;
+  const int g = lane >> 4, c = lane & 15;
+  const int G = a.Hq / a.Hkv;
+  const int n = a.decode ? 1 : s.qe - s.qs, rows = n * G;
+  if (rows <= 0) return;                         // the merge skips the session too
+  int64_t before = 0;
+  if (a.decode) before = b;
+  else
+    for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
+  // row r: head r / n of the group, token r % n; rows past the last repeat it and are not written
+  const int r = min(c, rows - 1), h = r / n, t = r - h * n;
+  const int64_t q_at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D;
+
+  // entries seen by any token: the first `skip` ... no more than the sinks, then [lo, N)
+  const int N = max(0, min(a.n_live[b], s.N)), own = N - n + t;
+  const int lo = a.window ? max(0, N - n - a.window + 1) : 0;
+  const int first = min(a.sinks, lo), gap = lo - first;        // index v stands for entry v, or v + gap from `first` on
+  const int T = N - gap;
+  const int chunk = ((T + nsplit - 1) / nsplit + 15) & ~15;
+  const int v0 = min(T, split * chunk), v1 = min(T, v0 + chunk);
+
+  float m = -INFINITY, lsum = 0.f;               // reference of row c; this lane's sum of weights
+  f32x4_k o[NC];                                 // o[j][i]: channel NC (4 g + i) + j of row c
+#pragma unroll
+  for (int j = 0; j < NC; ++j) o[j] = f32x4_k{0.f, 0.f, 0.f, 0.f};
+
+  if (v0 < v1) {
+    // queries as the B operand, channels in the order the key loads have them
+    bf16x8_k qf[KS][QP];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int ch = FMT == KV_BF16 ? 32 * ks + 8 * g : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
+      float x[8];
+      load8(static_cast<const typename std::conditional<sizeof(IO) == 4, float, uint16_t>::type *>(a.q) + q_at + ch, x);
+      split_parts<QP>(x, qf[ks]);
+    }
+    const int64_t row_bytes = int64_t(a.Hkv) * D * ES;
+    const int64_t layer = int64_t(l) * a.num_slots;
+    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES + 16 * g;
+    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES + c * (NC * ES);
+    const float2 *sbase = reinterpret_cast<const float2 *>(a.scales) + layer * a.Hkv + hkv;
+    const int32_t *list = a.live + s.slot_off;
+    const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
+
+    struct Block {
+      uint4 k[2][KW];
+      uint32_t v[8][VW];
+      float2 s;
+    };
+    // slot of index base + (lane & 31), the last index's past the end
+    auto slots = [&](int base) __attribute__((always_inline)) {
+      const int v = min(base + (lane & 31), v1 - 1);
+      return list[v < first ? v : v + gap];
+    };
+    auto load = [&](Block &x, int sl) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const char *p = kbase + int64_t(__builtin_amdgcn_ds_bpermute(4 * (16 * kb + c), sl)) * row_bytes;
+#pragma unroll
+        for (int j = 0; j < KW; ++j) x.k[kb][j] = *reinterpret_cast<const uint4 *>(p + 64 * j);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = e < 4 ? 4 * g + e : 16 + 4 * g + e - 4;
+        const char *p = vbase + int64_t(__builtin_amdgcn_ds_bpermute(4 * at, sl)) * row_bytes;
+        if constexpr (VW == 1) x.v[e][0] = *reinterpret_cast<const uint32_t *>(p);
+        else if constexpr (VW == 2) {
+          const uint2 y = *reinterpret_cast<const uint2 *>(p);
+          x.v[e][0] = y.x;
+          x.v[e][1] = y.y;
+        } else {
+          const uint4 y = *reinterpret_cast<const uint4 *>(p);
+          x.v[e][0] = y.x;
+          x.v[e][1] = y.y;
+          x.v[e][2] = y.z;
+          x.v[e][3] = y.w;
+        }
+      }
+      if constexpr (FMT != KV_BF16) x.s = sbase[int64_t(sl) * a.Hkv];
+    };
+    auto compute = [&](Block &x, int base, int sl) __attribute__((always_inline)) {
+      f32x4_k acc[2] = {f32x4_k{0.f, 0.f, 0.f, 0.f}, f32x4_k{0.f, 0.f, 0.f, 0.f}};
+      if constexpr (FMT != KV_BF16) {
+        if (lane < FEW_BLOCK) {
+          sc[w][0][lane] = x.s.x * to_log2;
+          sc[w][1][lane] = x.s.y;
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          uint4 u;
+          if constexpr (FMT == KV_BF16) u = x.k[kb][ks];
+          else {
+            const uint4 y = x.k[kb][ks >> 1];
+            const uint2 p = codes4<FMT>(ks & 1 ? y.z : y.x), q = codes4<FMT>(ks & 1 ? y.w : y.y);
+            u = make_uint4(p.x, p.y, q.x, q.y);
+          }
+          const bf16x8_k kf = __builtin_bit_cast(bf16x8_k, u);
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p) acc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks][p], acc[kb], 0, 0, 0);
+        }
+      float4 vs[2];
+      if constexpr (FMT != KV_BF16) {
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const float4 ks = *reinterpret_cast<const float4 *>(&sc[w][0][16 * kb + 4 * g]);
+          vs[kb] = *reinterpret_cast<const float4 *>(&sc[w][1][16 * kb + 4 * g]);
+          acc[kb][0] *= ks.x;
+          acc[kb][1] *= ks.y;
+          acc[kb][2] *= ks.z;
+          acc[kb][3] *= ks.w;
+        }
+        __builtin_amdgcn_wave_barrier();
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) acc[kb] *= to_log2;
+      }
+      // a block that every token sees whole needs no mask: its last entry is at or before the
+      // oldest token's own, and its first inside the newest's window or all of it among the sinks
+      const int last = base + FEW_BLOCK - 1, oldest = N - n;
+      const int jl = last < first ? last : last + gap, j0 = base < first ? base : base + gap;
+      const bool whole = last < v1 && jl <= oldest && (a.window == 0 || jl < a.sinks || j0 > N - 1 - a.window);
+      uint32_t hidden = 0;                         // bit 4 kb + i: not seen by this lane's row
+      if (!whole) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int v = base + 16 * kb + 4 * g + i, j = v < first ? v : v + gap;
+            const bool see = v < v1 && j <= own && (a.window == 0 || j < a.sinks || j > own - a.window);
+            if (!see) {
+              hidden |= 1u << (4 * kb + i);
+              acc[kb][i] = -INFINITY;
+            }
+          }
+      }
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, acc[kb][i]);
+      if (__builtin_amdgcn_ballot_w64(!(tmax - m <= FEW_SLACK)) != 0) {
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 16, WAVE));
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
+        const float mn = fmaxf(m, tmax);
+        const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        lsum *= corr;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) o[j] *= corr;
+      }
+      float pw[8];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float p = __builtin_amdgcn_exp2f(acc[kb][i] - m);
+          if (hidden >> (4 * kb + i) & 1) p = 0.f;
+          lsum += p;
+          if constexpr (FMT != KV_BF16) {
+            p *= (&vs[kb].x)[i];
+            if (hidden >> (4 * kb + i) & 1) p = 0.f;        // the scale of an unseen row may be anything
+          }
+          pw[4 * kb + i] = p;
+        }
+      // bf16 values that are not finite would turn the zero weights of rows that do not see
+      // them into NaN: such entries are taken out of the product and added row by row
+      uint32_t odd = 0;                            // bit e: this lane's entry e holds one
+      if constexpr (FMT == KV_BF16) {
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            bool f = false;
+#pragma unroll
+            for (int k = 0; k < VW; ++k) f |= (x.v[e][k] & 0x7f80u) == 0x7f80u || (x.v[e][k] & 0x7f800000u) == 0x7f800000u;
+            if (__builtin_amdgcn_ballot_w64(f) >> (16 * g) & 0xffffu) {
+              odd |= 1u << e;
+#pragma unroll
+              for (int k = 0; k < VW; ++k) x.v[e][k] = 0u;
+            }
+          }
+        }
+      }
+      bf16x8_k pf[PP];
+      split_parts<PP>(pw, pf);
+      // the operand of channels NC c + j .. + 3 (8-bit) or + 1 (bf16) at a time
+      constexpr int STEP = FMT == KV_BF16 ? 2 : 4;
+#pragma unroll
+      for (int k = 0; k < VW; ++k) {
+        uint32_t f[STEP][4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          if constexpr (FMT == KV_BF16) {
+            f[0][p] = __builtin_amdgcn_perm(x.v[2 * p + 1][k], x.v[2 * p][k], 0x05040100u);
+            f[1][p] = __builtin_amdgcn_perm(x.v[2 * p + 1][k], x.v[2 * p][k], 0x07060302u);
+          } else {
+            uint32_t y[4];
+            codes_across<FMT>(x.v[2 * p][k], x.v[2 * p + 1][k], y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i][p] = y[i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+          const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(f[i][0], f[i][1], f[i][2], f[i][3]));
+#pragma unroll
+          for (int p = PP - 1; p >= 0; --p)
+            o[STEP * k + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[p], o[STEP * k + i], 0, 0, 0);
+        }
+      }
+      if constexpr (FMT == KV_BF16) {
+        if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            for (int gg = 0; gg < 4; ++gg) {
+              if (!(__builtin_amdgcn_readlane(odd, 16 * gg) >> e & 1)) continue;
+              const float p = __shfl(pw[e], 16 * gg + c, WAVE);
+              const bool see = !(__shfl(hidden, 16 * gg + c, WAVE) >> e & 1);
+              const int at = e < 4 ? 4 * gg + e : 16 + 4 * gg + e - 4;
+              const uint16_t *row = reinterpret_cast<const uint16_t *>(
+                  static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES +
+                  int64_t(__builtin_amdgcn_readlane(sl, at)) * row_bytes);
+#pragma unroll
+              for (int j = 0; j < NC; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (see) o[j][i] = fmaf(p, Store<uint16_t>::ld(row + NC * (4 * g + i) + j), o[j][i]);
+            }
+        }
+      }
+    };
+    Block A, Bk;
+    int sa = slots(v0), sb = slots(v0 + FEW_BLOCK);
+    load(A, sa);
+    for (int base = v0; base < v1; base += 2 * FEW_BLOCK) {
+      const int s2 = slots(base + 2 * FEW_BLOCK), s3 = slots(base + 3 * FEW_BLOCK);
+      load(Bk, sb);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(A, base, sa);
+      __builtin_amdgcn_sched_barrier(0);
+      load(A, s2);
+      __builtin_amdgcn_sched_barrier(0);
+      if (base + FEW_BLOCK < v1) compute(Bk, base + FEW_BLOCK, sb);
+      sa = s2;
+      sb = s3;
+    }
+  }
+  lsum += __shfl_xor(lsum, 16, WAVE);
+  lsum += __shfl_xor(lsum, 32, WAVE);
+  if (c >= rows) return;
+  if (nsplit == 1) {
+    const float inv = m == -INFINITY ? 0.f : 1.0f / lsum;      // nothing seen: zero
+    IO *out = static_cast<IO *>(a.out) + q_at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NC; ++j) out[NC * (4 * g + i) + j] = Store<IO>::from(o[j][i] * inv);
+    return;
+  }
+  const int64_t part = (((int64_t(b) * a.L + l) * a.Hkv + hkv) * nsplit + split) * rows_max + c;
+  const int64_t parts = int64_t(gridDim.z) * a.L * a.Hkv * nsplit * rows_max;
+  float *po = a.ws + part * D;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < NC; j += 4)
+      *reinterpret_cast<float4 *>(po + NC * (4 * g + i) + j) = make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
+  if (g == 0) *reinterpret_cast<float2 *>(a.ws + parts * D + part * 2) = make_float2(m, lsum);
+}
+
+// The splits of a row: with M their largest reference, sum_z o_z 2^(m_z - M) over
+// sum_z l_z 2^(m_z - M); a split that saw nothing has m = -inf and weighs zero.
+template <typename IO, int D>
+__global__ void __launch_bounds__(D) k_attend_merge(AttendArgs a, int nsplit, int rows_max) {
+  __shared__ float sm[DEC_MAX_SPLITS], sl[DEC_MAX_SPLITS];
+  const int b = blockIdx.z, u = blockIdx.x, r = blockIdx.y, l = u / a.Hkv, hkv = u - l * a.Hkv;
+  const ikv_session s = a.sess[b];
+  const int n = a.decode ? 1 : s.qe - s.qs, G = a.Hq / a.Hkv;
+  if (r >= n * G) return;
+  int64_t before = 0;
+  if (a.decode) before = b;
+  else
+    for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
+  const int d = threadIdx.x;
+  const int64_t part = (int64_t(b) * gridDim.x + u) * nsplit * rows_max + r;
+  const int64_t parts = int64_t(gridDim.z) * gridDim.x * nsplit * rows_max;
+  if (d < nsplit) {
+    const float2 x = *reinterpret_cast<const float2 *>(a.ws + parts * D + (part + int64_t(d) * rows_max) * 2);
+    sm[d] = x.x;
+    sl[d] = x.y;
+  }
+  __syncthreads();
+  float M = -INFINITY;
+  for (int z = 0; z < nsplit; ++z) M = fmaxf(M, sm[z]);
+  float acc = 0.f, sum = 0.f;
+  if (M != -INFINITY)
+#pragma unroll 8
+    for (int z = 0; z < nsplit; ++z) {
+      const float x = a.ws[(part + int64_t(z) * rows_max) * D + d];
+      const float f = sm[z] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[z] - M);
+      acc = fmaf(x, f, acc);
+      sum = fmaf(sl[z], f, sum);
+    }
+  const int h = r / n, t = r - h * n;
+  const int64_t at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D + d;
+  static_cast<IO *>(a.out)[at] = Store<IO>::from(M == -INFINITY ? 0.f : acc / sum);
+}
+
+template <int FMT, typename IO, int D>
+static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  {
+    KTimer kt_("k_attend_few", st);
+    k_attend_few<FMT, IO, D><<<dim3(p.splits, a.L * (a.Hkv / p.heads), a.B), 64 * p.heads, 0, st>>>(a, p.rows);
+  }
+  if (p.splits > 1) {
+    KTimer kt_("k_attend_merge", st);
+    k_attend_merge<IO, D><<<dim3(a.L * a.Hkv, p.rows, a.B), D, 0, st>>>(a, p.splits, p.rows);
+  }
+}
+
+template <int FMT, typename IO>
+static void go_few_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  a.D == 128 ? go_few<FMT, IO, 128>(a, p, st) : go_few<FMT, IO, 64>(a, p, st);
+}
+
+hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if (a.format == KV_BF16) go_few_d<KV_BF16, uint16_t>(a, p, st);
+  else if (a.format == KV_INT8) a.io_f32 ? go_few_d<KV_INT8, float>(a, p, st) : go_few_d<KV_INT8, uint16_t>(a, p, st);
+  else a.io_f32 ? go_few_d<KV_E4M3, float>(a, p, st) : go_few_d<KV_E4M3, uint16_t>(a, p, st);
+  return hipGetLastError();
+}
+
+}  // namespace ikv

@@ -1,0 +1,46 @@
+// 8-bit codes as bf16 matrix operands. Both codes are exact in bf16: an int8 has 7
+// significant bits, an E4M3 value 4.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attend.hpp"
+
+namespace ikv {
+
+typedef __bf16 bf16x8_k __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_k __attribute__((ext_vector_type(2)));
+typedef float f32x4_k __attribute__((ext_vector_type(4)));
+
+// Two values exact in bf16, packed (the upper halves of their float32 bits).
+__device__ __forceinline__ uint32_t pack_exact(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+__device__ __forceinline__ float int8_at(uint32_t w, int byte) { return float(int8_t(w >> (8 * byte))); }
+template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+}
+
+// 4 adjacent codes of a word -> 4 bf16.
+template <int FMT> __device__ __forceinline__ uint2 codes4(uint32_t w) {
+  if constexpr (FMT == KV_E4M3) return make_uint2(e4m3_pair<false>(w), e4m3_pair<true>(w));
+  else return make_uint2(pack_exact(int8_at(w, 0), int8_at(w, 1)), pack_exact(int8_at(w, 2), int8_at(w, 3)));
+}
+
+// One word of two rows (4 adjacent channels each) -> for each of the 4 channels, the bf16
+// pair (row a, row b).
+template <int FMT> __device__ __forceinline__ void codes_across(uint32_t a, uint32_t b, uint32_t (&o)[4]) {
+  if constexpr (FMT == KV_E4M3) {
+    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u), hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
+    o[0] = e4m3_pair<false>(lo);
+    o[1] = e4m3_pair<true>(lo);
+    o[2] = e4m3_pair<false>(hi);
+    o[3] = e4m3_pair<true>(hi);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = pack_exact(int8_at(a, i), int8_at(b, i));
+  }
+}
+
+}  // namespace ikv
