@@ -23,7 +23,8 @@ ARCH = "gfx950"
 
 SOURCES = ["ikv_api.hip", "k_memory.hip", "k_score.hip", "k_score_mfma.hip", "k_score_narrow.hip", "k_residual.hip",
            "k_residual_mfma.hip", "k_select.hip", "k_decode.hip", "k_compact.hip", "k_prefill.hip",
-           "k_quant.hip", "k_attend.hip", "k_attend_few.hip", "ikv_session.cpp"]
+           "k_quant.hip", "k_attend.hip", "k_attend_few.hip", "k_attend_tile.hip",
+           "ikv_session.cpp"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",

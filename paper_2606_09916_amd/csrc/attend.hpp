@@ -33,6 +33,7 @@ struct AttendArgs {
 
 constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all
 constexpr int FEW_ROUND = 1024;     // workgroups of one resident round of k_attend_few
+constexpr int TILE_KEYS = 64;       // entries per tile of k_attend_tile
 
 struct AttendPlan {
   int max_n;               // longest chunk of the batch
@@ -40,7 +41,8 @@ struct AttendPlan {
   bool few;                // every session's rows per KV head fit one 16-row block
   int heads;               // adjacent KV heads of a workgroup (few)
   int splits;              // of the entries of a session
-  int rows;                // rows per (session, layer, KV head) in the split state
+  int blocks;              // row blocks per (session, layer, KV head): one (few)
+  int rows;                // rows per block in the split state
   int64_t ws_floats;
 };
 
@@ -63,7 +65,7 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     longest = std::max(longest, len);
   }
   p.few = int64_t(p.max_n) * G <= FEW_ROWS;
-  p.splits = 1;
+  p.splits = p.blocks = 1;
   if (p.few) {
     p.rows = p.max_n * G;
     p.heads = a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1;
@@ -71,9 +73,18 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     int64_t s = std::max<int64_t>(1, FEW_ROUND / wgs);
     s = std::min<int64_t>(s, (longest + 127) / 128);
     p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
-    if (p.splits > 1) p.ws_floats = int64_t(B) * a.L * a.Hkv * p.splits * p.rows * (a.D + 2);
+  } else if (p.max_n > 0) {
+    const int64_t rows = int64_t(p.max_n) * G;
+    p.rows = rows <= 128 ? 128 : 256;
+    p.blocks = int(std::min<int64_t>((rows + p.rows - 1) / p.rows, INT32_MAX));
+    const int64_t wgs = int64_t(a.L) * a.Hkv * B * p.blocks;
+    int64_t s = std::max<int64_t>(1, 1024 / wgs);
+    s = std::min<int64_t>(s, (longest + 511) / 512);
+    p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
   }
-  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535;
+  const int64_t parts = int64_t(B) * a.L * a.Hkv * p.blocks * p.splits * p.rows;
+  if (p.splits > 1) p.ws_floats = parts * (a.D + 2);
+  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || int64_t(B) * a.L * a.Hkv * p.blocks > (1 << 24);
   return p;
 }
 

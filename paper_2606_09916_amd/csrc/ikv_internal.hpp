@@ -327,6 +327,8 @@ hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const 
 hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
                              const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
+hipError_t launch_attend_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
+hipError_t launch_attend_merge(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 
 // A word of pinned host memory that kernels set (system scope) to report a fault the

@@ -71,8 +71,8 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
   if (a.decode) before = b;
   else
     for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
-  // row r: head r / n of the group, token r % n; rows past the last repeat it and are not written
-  const int r = min(c, rows - 1), h = r / n, t = r - h * n;
+  // row r: token r / G, head r % G of the group; rows past the last repeat it and are not written
+  const int r = min(c, rows - 1), t = r / G, h = r - t * G;
   const int64_t q_at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D;
 
   // entries seen by any token: the first `skip` ... no more than the sinks, then [lo, N)
@@ -336,54 +336,10 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
   if (g == 0) *reinterpret_cast<float2 *>(a.ws + parts * D + part * 2) = make_float2(m, lsum);
 }
 
-// The splits of a row: with M their largest reference, sum_z o_z 2^(m_z - M) over
-// sum_z l_z 2^(m_z - M); a split that saw nothing has m = -inf and weighs zero.
-template <typename IO, int D>
-__global__ void __launch_bounds__(D) k_attend_merge(AttendArgs a, int nsplit, int rows_max) {
-  __shared__ float sm[DEC_MAX_SPLITS], sl[DEC_MAX_SPLITS];
-  const int b = blockIdx.z, u = blockIdx.x, r = blockIdx.y, l = u / a.Hkv, hkv = u - l * a.Hkv;
-  const ikv_session s = a.sess[b];
-  const int n = a.decode ? 1 : s.qe - s.qs, G = a.Hq / a.Hkv;
-  if (r >= n * G) return;
-  int64_t before = 0;
-  if (a.decode) before = b;
-  else
-    for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
-  const int d = threadIdx.x;
-  const int64_t part = (int64_t(b) * gridDim.x + u) * nsplit * rows_max + r;
-  const int64_t parts = int64_t(gridDim.z) * gridDim.x * nsplit * rows_max;
-  if (d < nsplit) {
-    const float2 x = *reinterpret_cast<const float2 *>(a.ws + parts * D + (part + int64_t(d) * rows_max) * 2);
-    sm[d] = x.x;
-    sl[d] = x.y;
-  }
-  __syncthreads();
-  float M = -INFINITY;
-  for (int z = 0; z < nsplit; ++z) M = fmaxf(M, sm[z]);
-  float acc = 0.f, sum = 0.f;
-  if (M != -INFINITY)
-#pragma unroll 8
-    for (int z = 0; z < nsplit; ++z) {
-      const float x = a.ws[(part + int64_t(z) * rows_max) * D + d];
-      const float f = sm[z] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[z] - M);
-      acc = fmaf(x, f, acc);
-      sum = fmaf(sl[z], f, sum);
-    }
-  const int h = r / n, t = r - h * n;
-  const int64_t at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D + d;
-  static_cast<IO *>(a.out)[at] = Store<IO>::from(M == -INFINITY ? 0.f : acc / sum);
-}
-
 template <int FMT, typename IO, int D>
 static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  {
-    KTimer kt_("k_attend_few", st);
-    k_attend_few<FMT, IO, D><<<dim3(p.splits, a.L * (a.Hkv / p.heads), a.B), 64 * p.heads, 0, st>>>(a, p.rows);
-  }
-  if (p.splits > 1) {
-    KTimer kt_("k_attend_merge", st);
-    k_attend_merge<IO, D><<<dim3(a.L * a.Hkv, p.rows, a.B), D, 0, st>>>(a, p.splits, p.rows);
-  }
+  KTimer kt_("k_attend_few", st);
+  k_attend_few<FMT, IO, D><<<dim3(p.splits, a.L * (a.Hkv / p.heads), a.B), 64 * p.heads, 0, st>>>(a, p.rows);
 }
 
 template <int FMT, typename IO>
@@ -395,7 +351,7 @@ hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream
   if (a.format == KV_BF16) go_few_d<KV_BF16, uint16_t>(a, p, st);
   else if (a.format == KV_INT8) a.io_f32 ? go_few_d<KV_INT8, float>(a, p, st) : go_few_d<KV_INT8, uint16_t>(a, p, st);
   else a.io_f32 ? go_few_d<KV_E4M3, float>(a, p, st) : go_few_d<KV_E4M3, uint16_t>(a, p, st);
-  return hipGetLastError();
+  return p.splits > 1 ? launch_attend_merge(a, p, st) : hipGetLastError();
 }
 
 }  // namespace ikv

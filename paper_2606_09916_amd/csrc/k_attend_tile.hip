@@ -1,0 +1,418 @@
+// Attention of a chunk of new tokens: blocks of query rows against tiles of 64 entries.
+//
+// Row R of a KV head is (token R / G, head R % G of the group): a workgroup takes NW x 32
+// consecutive rows, so the G heads of a token share every key and value read, and a block's
+// tokens are neighbours with nearly the same entries to see. Bound by the matrix cores and,
+// beside them, the vector unit's work per logit.
+//   staging   rows or codes go from HBM to registers two tiles ahead, are made bf16 (codes
+//             exactly) and written to one of two LDS buffers: keys [64][D + 8], values
+//             [64][D + 32] (D = 64: + 32), strides that spread the reads below over all banks
+//   S^T = K Q^T with 32 x 32 x 16 products: lane (h, c) holds entries 8 i + 4 h + (0..3) of
+//             row c, so a row's softmax is two lanes' business
+//   softmax   a reference per row that moves only when a logit is TILE_SLACK above it (the
+//             weights stay below 2^8; most tiles exchange nothing between lanes)
+//   O^T += V^T P^T: the contraction's order is free, so the weights a lane holds are its
+//             operand as they are; the transposing LDS reads (4 entries x 16 channels by 16
+//             lanes) bring the value operand in that order from row-major tiles.
+// Weights are rounded to bf16 for bf16 outputs (2^-8 each, no more than the output's own
+// rounding, and averaged over the entries; their sum is of the unrounded ones). float32
+// outputs take queries and weights as three bf16 parts.
+#include <math.h>
+
+#include <type_traits>
+
+#include "attend.hpp"
+#include "ikv_internal.hpp"
+#include "kv_codes.hpp"
+
+namespace ikv {
+
+typedef float f32x16_k __attribute__((ext_vector_type(16)));
+typedef short s16x4_k __attribute__((ext_vector_type(4)));
+
+constexpr float TILE_SLACK = 8.f;                // log2
+
+__device__ __forceinline__ uint2 read_tr16(const uint16_t *p) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_k *)p));
+}
+
+// 8 floats as PARTS bf16 operands (nearest, then the nearest of what is left).
+template <int PARTS>
+__device__ __forceinline__ void tile_parts(const float *x, bf16x8_k (&o)[PARTS]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float r = x[e];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      o[p][e] = __bf16(r);
+      if (p + 1 < PARTS) r -= float(o[p][e]);
+    }
+  }
+}
+
+template <int FMT, typename IO, int D, int NW>
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
+k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
+  constexpr int ES = FMT == KV_BF16 ? 2 : 1;
+  constexpr int NT = 64 * NW, ROWS = 32 * NW;
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int KROW = D + 8, VROW = D + 32;
+  constexpr int PPR = D * ES / 16;               // 16-byte pieces of a row
+  constexpr int PIECES = TILE_KEYS * PPR;        // of a tile's keys (as many of its values)
+  constexpr int PT = 2 * PIECES / NT;            // pieces of a thread: keys first, then values
+  constexpr int QP = sizeof(IO) == 4 ? 3 : 1, PP = QP;
+  static_assert(2 * PIECES % NT == 0 && (PIECES % NT == 0 || NT % PIECES == 0), "whole pieces");
+  __shared__ __align__(16) uint16_t ks_[2][TILE_KEYS * KROW];
+  __shared__ __align__(16) uint16_t vs_[2][TILE_KEYS * VROW];
+  __shared__ __align__(16) float sc_[2][2][TILE_KEYS];               // scales: keys' (times log2 e / sqrt D), values'
+  __shared__ __align__(16) uint8_t odd_[2][FMT == KV_BF16 ? TILE_KEYS * PPR : 16];   // pieces with a value not finite
+
+  // units (session, layer, KV head) in steps of 8, so that a unit's blocks and splits run on
+  // one XCD and share its rows in that L2; the blocks with the most entries first
+  const int per = blocks * nsplit;
+  const int id = blockIdx.x, in = (id >> 3) % per, unit = (id >> 3) / per * 8 + (id & 7);
+  if (unit >= units) return;
+  const int rb = blocks - 1 - in / nsplit, split = in % nsplit;
+  const int hkv = unit % a.Hkv, l = unit / a.Hkv % a.L, b = unit / a.Hkv / a.L;
+  const ikv_session s = a.sess[b];
+  const int G = a.Hq / a.Hkv, n = a.decode ? 1 : s.qe - s.qs, rows = n * G;
+  const int row0 = rb * ROWS;
+  if (row0 >= rows) return;
+  int64_t before = 0;
+  if (a.decode) before = b;
+  else
+    for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h2 = lane >> 5, c = lane & 31;
+  const int row = row0 + 32 * w + c, rr = min(row, rows - 1);
+  const int t = rr / G, h = rr - t * G;
+  const int64_t q_at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D;
+
+  // what the block sees: up to the sinks, then [lo, own of its newest token]
+  const int N = max(0, min(a.n_live[b], s.N)), own = N - n + t;
+  const int t0 = row0 / G, t1 = min(rows - 1, row0 + ROWS - 1) / G;
+  const int own0 = N - n + t0, own1 = N - n + t1;
+  const int lo = a.window ? max(0, own0 - a.window + 1) : 0;
+  const int first = min(a.sinks, lo), gap = lo - first;        // index v stands for entry v, or v + gap from `first` on
+  const int T = max(0, own1 + 1 - gap);
+  const int ntile = (T + TILE_KEYS - 1) / TILE_KEYS;
+  const int tb = int(int64_t(ntile) * split / nsplit), te = int(int64_t(ntile) * (split + 1) / nsplit);
+  // this wave's tokens
+  const int wrow0 = min(row0 + 32 * w, rows - 1), wrow1 = min(row0 + 32 * w + 31, rows - 1);
+  const int wown0 = N - n + wrow0 / G, wown1 = N - n + wrow1 / G;
+  const bool wave_on = row0 + 32 * w < rows;
+
+  float m = -INFINITY, lsum = 0.f;
+  f32x16_k o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+
+  if (tb < te) {
+    bf16x8_k qf[KS][QP];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float x[8];
+      load8(static_cast<const typename std::conditional<sizeof(IO) == 4, float, uint16_t>::type *>(a.q) + q_at + 16 * ks +
+                8 * h2, x);
+      tile_parts<QP>(x, qf[ks]);
+    }
+    const int64_t row_bytes = int64_t(a.Hkv) * D * ES;
+    const int64_t layer = int64_t(l) * a.num_slots;
+    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES;
+    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES;
+    const float2 *sbase = reinterpret_cast<const float2 *>(a.scales) + layer * a.Hkv + hkv;
+    const int32_t *list = a.live + s.slot_off;
+    const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
+
+    struct Slots { int32_t s[PT], sc; };
+    struct Regs { uint4 r[PT]; float2 sc; };
+    auto entry = [&](int v) __attribute__((always_inline)) {
+      v = min(v, T - 1);                           // past the end the last one again, masked
+      return v < first ? v : v + gap;
+    };
+    auto slots = [&](int tile) __attribute__((always_inline)) {
+      Slots x;
+#pragma unroll
+      for (int i = 0; i < PT; ++i) x.s[i] = list[entry(tile * TILE_KEYS + (tid + i * NT) % PIECES / PPR)];
+      x.sc = FMT == KV_BF16 ? 0 : list[entry(tile * TILE_KEYS + lane)];
+      return x;
+    };
+    auto load = [&](const Slots &x, Regs &r) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int p = tid + i * NT;
+        r.r[i] = *reinterpret_cast<const uint4 *>((p < PIECES ? kbase : vbase) + int64_t(x.s[i]) * row_bytes +
+                                                  p % PPR * 16);
+      }
+      if constexpr (FMT != KV_BF16) r.sc = sbase[int64_t(x.sc) * a.Hkv];
+    };
+    // whether some token of [o0, o1] does not see all of the tile's entries
+    auto edge = [&](int tile, int o0, int o1) __attribute__((always_inline)) {
+      const int va = tile * TILE_KEYS, vb = va + TILE_KEYS - 1;
+      const int ja = va < first ? va : va + gap, jb = vb < first ? vb : vb + gap;
+      return !(vb < T && jb <= o0 && (a.window == 0 || jb < a.sinks || ja > o1 - a.window));
+    };
+    auto store = [&](int buf, const Regs &r, int tile) __attribute__((always_inline)) {
+      const bool look = FMT == KV_BF16 && edge(tile, own0, own1);
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int p = tid + i * NT, q = p % PIECES, key = q / PPR, at = q % PPR;
+        const bool isv = p >= PIECES;
+        uint16_t *dst = isv ? &vs_[buf][key * VROW] : &ks_[buf][key * KROW];
+        uint4 x = r.r[i];
+        if constexpr (FMT == KV_BF16) {
+          // a value that is not finite would turn the zero weights of rows that do not see it
+          // into NaN: it is left out here and added row by row
+          if (look && isv) {
+            uint32_t u[4] = {x.x, x.y, x.z, x.w};
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if ((u[k] & 0x7f80u) == 0x7f80u) odd = true, u[k] &= 0xffff0000u;
+              if ((u[k] & 0x7f800000u) == 0x7f800000u) odd = true, u[k] &= 0x0000ffffu;
+            }
+            x = make_uint4(u[0], u[1], u[2], u[3]);
+            odd_[buf][q] = odd;
+          }
+          *reinterpret_cast<uint4 *>(dst + at * 8) = x;
+        } else {
+          const uint2 p0 = codes4<FMT>(x.x), p1 = codes4<FMT>(x.y), p2 = codes4<FMT>(x.z), p3 = codes4<FMT>(x.w);
+          *reinterpret_cast<uint4 *>(dst + at * 16) = make_uint4(p0.x, p0.y, p1.x, p1.y);
+          *reinterpret_cast<uint4 *>(dst + at * 16 + 8) = make_uint4(p2.x, p2.y, p3.x, p3.y);
+        }
+      }
+      if constexpr (FMT != KV_BF16) {
+        if (tid < TILE_KEYS) {
+          sc_[buf][0][tid] = r.sc.x * to_log2;
+          sc_[buf][1][tid] = r.sc.y;
+        }
+      }
+    };
+    auto compute = [&](int buf, int tile) __attribute__((always_inline)) {
+      // nothing of the tile for this wave: past its newest token, or before its window and after the sinks
+      const int va = tile * TILE_KEYS, vb = va + TILE_KEYS - 1;
+      const int ja = va < first ? va : va + gap, jb = vb < first ? vb : vb + gap;
+      if (!wave_on || ja > wown1 || (a.window && ja >= a.sinks && jb <= wown0 - a.window)) return;
+      f32x16_k acc[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[kb][i] = 0.f;
+        const uint16_t *kr = &ks_[buf][(32 * kb + c) * KROW + 8 * h2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const bf16x8_k kf = *reinterpret_cast<const bf16x8_k *>(kr + 16 * ks);
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p)
+            acc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][p], acc[kb], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          if constexpr (FMT != KV_BF16) {
+            const float4 ks = *reinterpret_cast<const float4 *>(&sc_[buf][0][32 * kb + 8 * i4 + 4 * h2]);
+            acc[kb][4 * i4] *= ks.x;
+            acc[kb][4 * i4 + 1] *= ks.y;
+            acc[kb][4 * i4 + 2] *= ks.z;
+            acc[kb][4 * i4 + 3] *= ks.w;
+          }
+        }
+      const bool part = edge(tile, wown0, wown1);
+      uint32_t hidden = 0;                         // bit 16 kb + i: not seen by this lane's row
+      if (part) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int v = va + 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3), j = v < first ? v : v + gap;
+            const bool see = v < T && j <= own && (a.window == 0 || j < a.sinks || j > own - a.window);
+            if (!see) {
+              hidden |= 1u << (16 * kb + i);
+              acc[kb][i] = -INFINITY;
+            }
+          }
+      }
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, acc[kb][i]);
+      if constexpr (FMT == KV_BF16) tmax *= to_log2;
+      if (__builtin_amdgcn_ballot_w64(!(tmax - m <= TILE_SLACK)) != 0) {
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
+        const float mn = fmaxf(m, tmax);
+        const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        lsum *= corr;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= corr;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          acc[kb][i] = __builtin_amdgcn_exp2f(FMT == KV_BF16 ? fmaf(acc[kb][i], to_log2, -m) : acc[kb][i] - m);
+        }
+      if (part) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (hidden >> (16 * kb + i) & 1) acc[kb][i] = 0.f;
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += acc[kb][i];
+      lsum += sum;
+      if constexpr (FMT != KV_BF16) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const float4 vs = *reinterpret_cast<const float4 *>(&sc_[buf][1][32 * kb + 8 * i4 + 4 * h2]);
+            acc[kb][4 * i4] *= vs.x;
+            acc[kb][4 * i4 + 1] *= vs.y;
+            acc[kb][4 * i4 + 2] *= vs.z;
+            acc[kb][4 * i4 + 3] *= vs.w;
+          }
+        if (part) {                                // the scale of an unseen row may be anything
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (hidden >> (16 * kb + i) & 1) acc[kb][i] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = acc[st >> 1][8 * (st & 1) + e];
+        bf16x8_k pf[PP];
+        tile_parts<PP>(x, pf);
+        const int lr = lane & 15;
+        const uint16_t *vr = &vs_[buf][(16 * st + 4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3)];
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const uint2 x0 = read_tr16(vr + 32 * db), x1 = read_tr16(vr + 8 * VROW + 32 * db);
+          const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(x0.x, x0.y, x1.x, x1.y));
+#pragma unroll
+          for (int p = PP - 1; p >= 0; --p) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[p], o[db], 0, 0, 0);
+        }
+      }
+      if constexpr (FMT == KV_BF16) {
+        if (edge(tile, own0, own1)) {              // the values left out of the tile
+          uint32_t f = 0;
+#pragma unroll
+          for (int k = 0; k < PPR / 4; ++k) f |= reinterpret_cast<const uint32_t *>(&odd_[buf][lane * PPR])[k];
+          uint64_t todo = __builtin_amdgcn_ballot_w64(f != 0);
+          while (todo) {
+            const int key = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const uint16_t *vrow =
+                reinterpret_cast<const uint16_t *>(vbase + int64_t(list[entry(va + key)]) * row_bytes);
+            const int kb = key >> 5, hk = key >> 2 & 1, i = 4 * (key >> 3 & 3) + (key & 3);
+            float p = 0.f;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) p = k == 16 * kb + i ? acc[k >> 4][k & 15] : p;
+            p = __shfl(p, 32 * hk + c, WAVE);
+            const bool see = !(__shfl(hidden, 32 * hk + c, WAVE) >> (16 * kb + i) & 1);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
+                if (see && (y & 0x7f80u) == 0x7f80u) o[db][k] = fmaf(p, Store<uint16_t>::ld(&y), o[db][k]);
+              }
+          }
+        }
+      }
+    };
+    Regs rA, rB;
+    load(slots(tb), rA);
+    Slots s1 = slots(tb + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    load(s1, rB);
+    store(0, rA, tb);
+    Slots s2 = slots(tb + 2);
+    __syncthreads();
+    for (int tile = tb; tile < te; tile += 2) {
+      // buffer 0 holds `tile`, rB tile + 1
+      const Slots s3 = slots(tile + 3);
+      load(s2, rA);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(0, tile);
+      store(1, rB, tile + 1);
+      __syncthreads();
+      if (tile + 1 >= te) break;
+      s2 = slots(tile + 4);
+      load(s3, rB);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(1, tile + 1);
+      store(0, rA, tile + 2);
+      __syncthreads();
+    }
+  }
+  lsum += __shfl_xor(lsum, 32, WAVE);
+  if (row >= rows) return;
+  if (nsplit == 1) {
+    const float inv = m == -INFINITY ? 0.f : 1.0f / lsum;      // nothing seen: zero
+    IO *out = static_cast<IO *>(a.out) + q_at;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int ch = 32 * db + 8 * i4 + 4 * h2;
+        if constexpr (sizeof(IO) == 4) {
+          *reinterpret_cast<float4 *>(out + ch) = make_float4(o[db][4 * i4] * inv, o[db][4 * i4 + 1] * inv,
+                                                              o[db][4 * i4 + 2] * inv, o[db][4 * i4 + 3] * inv);
+        } else {
+          uint32_t u[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[i] = float_to_bf16_bits(o[db][4 * i4 + i] * inv);
+          *reinterpret_cast<uint2 *>(out + ch) = make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
+        }
+      }
+    return;
+  }
+  // split state, as the merge reads it: blocks of ROWS rows per (unit, block, split)
+  const int64_t at = ((int64_t(unit) * blocks + rb) * nsplit + split) * ROWS + 32 * w + c;
+  const int64_t parts = int64_t(units) * blocks * nsplit * ROWS;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4)
+      *reinterpret_cast<float4 *>(a.ws + at * D + 32 * db + 8 * i4 + 4 * h2) =
+          make_float4(o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]);
+  if (h2 == 0) *reinterpret_cast<float2 *>(a.ws + parts * D + at * 2) = make_float2(m, lsum);
+}
+
+template <int FMT, typename IO, int D, int NW>
+static void go_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  const int units = a.B * a.L * a.Hkv;
+  KTimer kt_("k_attend_tile", st);
+  k_attend_tile<FMT, IO, D, NW><<<dim3(unsigned((units + 7) / 8 * 8 * p.blocks * p.splits)), 64 * NW, 0, st>>>(
+      a, p.blocks, p.splits, units);
+}
+
+template <int FMT, typename IO>
+static hipError_t go_tile_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if (a.D == 128) p.rows == 256 ? go_tile<FMT, IO, 128, 8>(a, p, st) : go_tile<FMT, IO, 128, 4>(a, p, st);
+  else p.rows == 256 ? go_tile<FMT, IO, 64, 8>(a, p, st) : go_tile<FMT, IO, 64, 4>(a, p, st);
+  return p.splits > 1 ? launch_attend_merge(a, p, st) : hipGetLastError();
+}
+
+hipError_t launch_attend_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+  if (a.format == KV_BF16) return go_tile_d<KV_BF16, uint16_t>(a, p, st);
+  if (a.format == KV_INT8) return a.io_f32 ? go_tile_d<KV_INT8, float>(a, p, st) : go_tile_d<KV_INT8, uint16_t>(a, p, st);
+  return a.io_f32 ? go_tile_d<KV_E4M3, float>(a, p, st) : go_tile_d<KV_E4M3, uint16_t>(a, p, st);
+}
+
+}  // namespace ikv
