@@ -1,7 +1,7 @@
 // Rows between a pool (bf16 or float32) and the 8-bit cache, by slot lists.
 //
 // A row (one layer, slot and KV head; K or V) of D channels belongs to D / 8 adjacent
-// lanes, 8 channels each: a list entry's K and V rows of one layer are 2 Hkv D / 8 threads.
+// lanes, 8 channels each.
 // With a = max(max|x|, 2^-100):
 //   int8  code = 127 x / a to the nearest whole number, ties to even, of the exact quotient.
 //         bf16 rows often meet exact ties (x = a / 2 gives 63.5), where a product with a
@@ -13,6 +13,8 @@
 //         (ties missed by no less than 2^-33).
 //   e4m3  scale = 2^e with 448 2^e >= a > 224 2^e: x / scale is exact, and the conversion
 //         rounds once.
+#include <algorithm>
+
 #include "ikv_internal.hpp"
 
 namespace ikv {
@@ -87,78 +89,77 @@ __device__ __forceinline__ uint2 quant8(const float (&x)[8], uint32_t amax_bits,
   return make_uint2(w[0], w[1]);
 }
 
-// Thread's place: list entry k of the session, then (K or V, head, 8-channel piece).
-struct QuantPlace {
-  int k, kv, row, piece;                         // row = head; piece of 8 channels
-};
-__device__ __forceinline__ QuantPlace quant_place(int64_t idx, int Hkv, int lpr) {
-  const int per = 2 * Hkv * lpr;
-  QuantPlace p;
-  p.k = int(idx / per);
-  const int r = int(idx - int64_t(p.k) * per);
-  p.kv = r >= Hkv * lpr;
-  const int q = r - p.kv * Hkv * lpr;
-  p.row = q / lpr;
-  p.piece = q - p.row * lpr;
-  return p;
-}
-
 __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n_rows, int b) {
   return n_rows ? max(0, min(n_rows[b], s.N)) : s.N;
 }
+
+// A workgroup takes `group` list entries of one layer; an entry is `per` = Hkv D / 8 threads'
+// work, a thread's 8 channels of its K and of its V row. A thread takes QU places at a time,
+// all their slots loaded first, then all their rows: bound by memory, the kernels need that
+// many bytes in flight per CU.
+constexpr int QU = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool, const T *__restrict__ vpool,
                                                     int64_t pool_slots, uint8_t *__restrict__ kc,
                                                     uint8_t *__restrict__ vc, float *__restrict__ scales,
-                                                    int64_t num_slots, int Hkv, int code, int dead,
+                                                    int64_t num_slots, int Hkv, int code, int dead, int group,
                                                     const ikv_session *__restrict__ sess,
                                                     const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
                                                     const int32_t *__restrict__ n_rows) {
   constexpr int LPR = D / 8;
-  const int l = blockIdx.y, b = blockIdx.z;
+  const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
   const ikv_session s = sess[b];
-  const QuantPlace p = quant_place(int64_t(blockIdx.x) * QT + threadIdx.x, Hkv, LPR);
-  if (p.k >= quant_rows(s, n_rows, b)) return;   // the lanes of a row leave together
-  const int64_t e = s.slot_off + p.k;
-  const int to = dst[e];
-  if (to == dead) return;
-  const int64_t from = src ? int64_t(src[e]) : e;
-  Row8<T> r;
-  r.ld((p.kv ? vpool : kpool) + ((int64_t(l) * pool_slots + from) * Hkv + p.row) * D + p.piece * 8);
-  float x[8];
-  r.get(x);
-  uint32_t m = 0;                                // |x| as bits: ordered, a NaN above infinity
+  const int k0 = blockIdx.x * group;
+  const int todo = min(group, quant_rows(s, n_rows, b) - k0) * per;
+  const int64_t e0 = s.slot_off + k0;
+  for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
+    Row8<T> rk[QU], rv[QU];
+    int64_t to[QU];
+    int at[QU];                                    // place within the entry's row; -1: none
+    int64_t from[QU];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int u = 0; u < QU; ++u) {
+      const int i = min(i0 + u * QT, todo - 1), k = i / per;
+      const int64_t e = e0 + k;
+      const int slot = dst[e];
+      at[u] = i0 + u * QT < todo && slot != dead ? i - k * per : -1;
+      to[u] = (int64_t(l) * num_slots + slot) * Hkv;
+      from[u] = ((int64_t(l) * pool_slots + (src ? int64_t(src[e]) : e)) * Hkv) * D + (i - k * per) * 8;
+    }
 #pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
-  float scale;
-  const uint2 w = quant8<T>(x, m, code, &scale);
-  const int64_t row = (int64_t(l) * num_slots + to) * Hkv + p.row;
-  *reinterpret_cast<uint2 *>((p.kv ? vc : kc) + row * D + p.piece * 8) = w;
-  if (p.piece == 0) scales[row * 2 + p.kv] = scale;
+    for (int u = 0; u < QU; ++u)
+      if (at[u] >= 0) {
+        rk[u].ld(kpool + from[u]);
+        rv[u].ld(vpool + from[u]);
+      }
+#pragma unroll
+    for (int u = 0; u < QU; ++u) {
+      if (at[u] < 0) continue;                     // the lanes of a row go together
+      uint2 w[2];
+      float sc[2];
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        float x[8];
+        (kv ? rv[u] : rk[u]).get(x);
+        uint32_t m = 0;                            // |x| as bits: ordered, a NaN above infinity
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
+        w[kv] = quant8<T>(x, m, code, &sc[kv]);
+      }
+      const int64_t row = to[u] + at[u] / LPR;
+      const int piece = at[u] % LPR;
+      *reinterpret_cast<uint2 *>(kc + row * D + piece * 8) = w[0];
+      *reinterpret_cast<uint2 *>(vc + row * D + piece * 8) = w[1];
+      if (piece == 0) reinterpret_cast<float2 *>(scales)[row] = make_float2(sc[0], sc[1]);
+    }
+  }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
-                                                   const float *__restrict__ scales, int64_t num_slots, int Hkv,
-                                                   int code, int dead, T *__restrict__ kpool, T *__restrict__ vpool,
-                                                   int64_t pool_slots, const ikv_session *__restrict__ sess,
-                                                   const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
-                                                   const int32_t *__restrict__ n_rows) {
-  constexpr int LPR = D / 8;
-  const int l = blockIdx.y, b = blockIdx.z;
-  const ikv_session s = sess[b];
-  const QuantPlace p = quant_place(int64_t(blockIdx.x) * QT + threadIdx.x, Hkv, LPR);
-  if (p.k >= quant_rows(s, n_rows, b)) return;
-  const int64_t e = s.slot_off + p.k;
-  const int from = src[e];
-  if (from == dead) return;
-  const int64_t to = dst ? int64_t(dst[e]) : e;
-  const int64_t row = (int64_t(l) * num_slots + from) * Hkv + p.row;
-  const uint2 w = *reinterpret_cast<const uint2 *>((p.kv ? vc : kc) + row * D + p.piece * 8);
-  const float scale = scales[row * 2 + p.kv];
+// 8 codes times their scale, to the pool's type.
+template <typename T> __device__ __forceinline__ void put8(T *o, uint2 w, float scale, int code) {
   const uint32_t u[2] = {w.x, w.y};
   float x[8];
 #pragma unroll
@@ -166,13 +167,66 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
     const int byte = int(u[i >> 2] >> (8 * (i & 3)));
     x[i] = (code == IKV_INT8 ? float(int8_t(byte)) : __builtin_amdgcn_cvt_f32_fp8(byte, 0)) * scale;
   }
-  T *o = (p.kv ? vpool : kpool) + ((int64_t(l) * pool_slots + to) * Hkv + p.row) * D + p.piece * 8;
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4 *>(o)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(o)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    bf16x8 y;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] = Store<T>::from(x[i]);
+    for (int i = 0; i < 8; ++i) y[i] = __bf16(x[i]);
+    *reinterpret_cast<bf16x8 *>(o) = y;
+  }
 }
 
+template <typename T, int D>
+__global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
+                                                   const float *__restrict__ scales, int64_t num_slots, int Hkv,
+                                                   int code, int dead, int group, T *__restrict__ kpool,
+                                                   T *__restrict__ vpool, int64_t pool_slots,
+                                                   const ikv_session *__restrict__ sess,
+                                                   const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
+                                                   const int32_t *__restrict__ n_rows) {
+  constexpr int LPR = D / 8;
+  const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
+  const ikv_session s = sess[b];
+  const int k0 = blockIdx.x * group;
+  const int todo = min(group, quant_rows(s, n_rows, b) - k0) * per;
+  const int64_t e0 = s.slot_off + k0;
+  for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
+    uint2 wk[QU], wv[QU];
+    float2 sc[QU];
+    int64_t to[QU], from[QU];
+    bool on[QU];
+#pragma unroll
+    for (int u = 0; u < QU; ++u) {
+      const int i = min(i0 + u * QT, todo - 1), k = i / per, at = i - k * per;
+      const int64_t e = e0 + k;
+      const int slot = src[e];
+      on[u] = i0 + u * QT < todo && slot != dead;
+      from[u] = (int64_t(l) * num_slots + slot) * per + at;                    // 8-code pieces
+      to[u] = ((int64_t(l) * pool_slots + (dst ? int64_t(dst[e]) : e)) * per + at) * 8;
+    }
+#pragma unroll
+    for (int u = 0; u < QU; ++u)
+      if (on[u]) {
+        wk[u] = reinterpret_cast<const uint2 *>(kc)[from[u]];
+        wv[u] = reinterpret_cast<const uint2 *>(vc)[from[u]];
+        sc[u] = reinterpret_cast<const float2 *>(scales)[from[u] / LPR];
+      }
+#pragma unroll
+    for (int u = 0; u < QU; ++u)
+      if (on[u]) {
+        put8(kpool + to[u], wk[u], sc[u].x, code);
+        put8(vpool + to[u], wv[u], sc[u].y, code);
+      }
+  }
+}
+
+// Entries of a workgroup: QU places per thread, one entry at least.
+static int quant_group(const ikv_quant_pool &c) { return std::max(1, QT * QU / (c.Hkv * (c.D / 8))); }
 static dim3 quant_grid(const ikv_quant_pool &c, int B, int maxN) {
-  return dim3(unsigned(cdiv(int64_t(maxN) * 2 * c.Hkv * (c.D / 8), QT)), unsigned(c.L), unsigned(B));
+  return dim3(unsigned(cdiv(maxN, quant_group(c))), unsigned(c.L), unsigned(B));
 }
 
 hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
@@ -183,7 +237,7 @@ hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const 
     using T = decltype(tag);
     kernel<<<grid, QT, 0, st>>>(static_cast<const T *>(p.k_pool), static_cast<const T *>(p.v_pool), p.num_slots,
                                 static_cast<uint8_t *>(c.k_codes), static_cast<uint8_t *>(c.v_codes), c.scales,
-                                c.num_slots, c.Hkv, c.code, c.dead_slot, sess_dev, src, dst, n_rows);
+                                c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), sess_dev, src, dst, n_rows);
   };
   if (p.kv_dtype == IKV_BF16) c.D == 128 ? go(uint16_t(), k_quant_store<uint16_t, 128>) : go(uint16_t(), k_quant_store<uint16_t, 64>);
   else c.D == 128 ? go(float(), k_quant_store<float, 128>) : go(float(), k_quant_store<float, 64>);
@@ -197,7 +251,7 @@ hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const i
   auto go = [&](auto tag, auto kernel) {
     using T = decltype(tag);
     kernel<<<grid, QT, 0, st>>>(static_cast<const uint8_t *>(c.k_codes), static_cast<const uint8_t *>(c.v_codes),
-                                c.scales, c.num_slots, c.Hkv, c.code, c.dead_slot, static_cast<T *>(p.k_pool),
+                                c.scales, c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), static_cast<T *>(p.k_pool),
                                 static_cast<T *>(p.v_pool), p.num_slots, sess_dev, src, dst, n_rows);
   };
   if (p.kv_dtype == IKV_BF16) c.D == 128 ? go(uint16_t(), k_quant_load<uint16_t, 128>) : go(uint16_t(), k_quant_load<uint16_t, 64>);

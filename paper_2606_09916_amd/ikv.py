@@ -136,27 +136,29 @@ def _stream(stream) -> int | None:
     return s.cuda_stream
 
 
-def _need(ok, status: int, func: str, msg: str) -> None:
-    if not ok:
-        raise IkvError(status, func, msg)
-
-
 def _tensor(t, dtype, numel: int, func: str, name: str) -> None:
     """A tensor argument as the kernels read it: this type, whole rows in order, at least this many elements."""
-    _need(t.dtype == dtype, -1, func, f"{name} is {t.dtype}, not {dtype}")
-    _need(t.is_contiguous(), -1, func, f"{name} is not contiguous")
-    _need(t.numel() >= numel, -2, func, f"{name} has {t.numel()} elements, {numel} needed")
+    if t.dtype != dtype:
+        raise IkvError(-1, func, f"{name} is {t.dtype}, not {dtype}")
+    if not t.is_contiguous():
+        raise IkvError(-1, func, f"{name} is not contiguous")
+    if t.numel() < numel:
+        raise IkvError(-2, func, f"{name} has {t.numel()} elements, {numel} needed")
 
 
-def _place(func: str, sess, stream, *tensors) -> None:
-    """Every tensor on the device of the stream that the call is enqueued on."""
+def _place(func: str, sess, stream, *tensors) -> int:
+    """The stream to enqueue on, once every tensor is on its device."""
     import torch
     dev = sess.dev.device
     for t in tensors:
-        _need(t is None or t.device == dev, -1, func, "tensors and sessions on different devices")
-    _need(dev.type == "cuda", -1, func, f"sessions are on {dev}, not on a GPU")
-    on = stream.device.index if stream is not None else torch.cuda.current_device()
-    _need(dev.index == on, -1, func, f"tensors are on {dev}, the stream is on cuda:{on}")
+        if t is not None and t.device != dev:
+            raise IkvError(-1, func, "tensors and sessions on different devices")
+    if dev.type != "cuda":
+        raise IkvError(-1, func, f"sessions are on {dev}, not on a GPU")
+    s = stream if stream is not None else torch.cuda.current_stream()
+    if dev != s.device:
+        raise IkvError(-1, func, f"tensors are on {dev}, the stream is on {s.device}")
+    return s.cuda_stream
 
 
 # ----------------------------------------------------------------------------- descriptors
@@ -176,8 +178,10 @@ def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slo
     code = {torch.int8: IKV_INT8, torch.float8_e4m3fn: IKV_E4M3}.get(k_codes.dtype)
     io = {None: IKV_BF16, torch.bfloat16: IKV_BF16, torch.float32: IKV_F32}.get(io_dtype)
     what = "make_quant_pool"
-    _need(code is not None, -1, what, f"codes of type {k_codes.dtype} (int8 or float8_e4m3fn)")
-    _need(io is not None, -1, what, f"io_dtype {io_dtype} (bfloat16 or float32)")
+    if code is None:
+        raise IkvError(-1, what, f"codes of type {k_codes.dtype} (int8 or float8_e4m3fn)")
+    if io is None:
+        raise IkvError(-1, what, f"io_dtype {io_dtype} (bfloat16 or float32)")
     rows = L * num_slots * Hkv
     _tensor(k_codes, k_codes.dtype, rows * D, what, "k_codes")
     _tensor(v_codes, k_codes.dtype, rows * D, what, "v_codes")
@@ -196,12 +200,12 @@ class Sessions:
         for i, r in enumerate(rows):
             for k, v in r.items():
                 setattr(self.host[i], k, int(v))
+        self.host_ptr = ctypes.cast(self.host, ctypes.POINTER(Session))
+        self.entries = max((x.slot_off + x.N for x in self.host[:self.B]), default=0)    # of the per-position arrays
+        self.span_tokens = sum(x.qe - x.qs for x in self.host[:self.B])
         raw = bytes(memoryview(self.host).cast("B"))[: self.B * ctypes.sizeof(Session)]
         self.dev = torch.frombuffer(bytearray(raw or b"\0"), dtype=torch.uint8).to(device)
 
-    @property
-    def host_ptr(self):
-        return ctypes.cast(self.host, ctypes.POINTER(Session))
 
     @property
     def dev_ptr(self) -> int:
@@ -317,10 +321,9 @@ def quant_workspace_bytes(cache: QuantPool, sess: Sessions, call: int) -> int:
 def _lists(sess: Sessions, ids, counts, func: str, names) -> None:
     """The per-entry slot lists (None where the call allows it) and the per-session counts."""
     import torch
-    total = max((sess.host[b].slot_off + sess.host[b].N for b in range(sess.B)), default=0)
     for t, name in zip(ids, names):
         if t is not None:
-            _tensor(t, torch.int32, total, func, name)
+            _tensor(t, torch.int32, sess.entries, func, name)
     if counts is not None:
         _tensor(counts, torch.int32, sess.B, func, "the counts")
 
@@ -328,17 +331,17 @@ def _lists(sess: Sessions, ids, counts, func: str, names) -> None:
 def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=None, stream=None) -> None:
     """Quantise rows of a pool into the 8-bit cache: slot src[k] (None: row slot_off + k) of the pool to slot dst[k]."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_store", ("src", "dst"))
-    _place("ikv_quant_store", sess, stream, src, dst, n_rows)
+    st = _place("ikv_quant_store", sess, stream, src, dst, n_rows)
     _check(lib().ikv_quant_store(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
-                                 _ptr(dst), _ptr(n_rows), _stream(stream)), "ikv_quant_store")
+                                 _ptr(dst), _ptr(n_rows), st), "ikv_quant_store")
 
 
 def quant_load(cache: QuantPool, pool: Pool, sess: Sessions, src, dst=None, n_rows=None, stream=None) -> None:
     """Read rows of the 8-bit cache back: slot src[k] of the cache to slot dst[k] (None: row slot_off + k) of the pool."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_load", ("src", "dst"))
-    _place("ikv_quant_load", sess, stream, src, dst, n_rows)
+    st = _place("ikv_quant_load", sess, stream, src, dst, n_rows)
     _check(lib().ikv_quant_load(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
-                                _ptr(dst), _ptr(n_rows), _stream(stream)), "ikv_quant_load")
+                                _ptr(dst), _ptr(n_rows), st), "ikv_quant_load")
 
 
 def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sinks: int, window: int, tokens: int, io,
@@ -349,13 +352,9 @@ def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sink
     _tensor(q, dt, numel, func, "q")
     _tensor(out, dt, numel, func, "out")
     _lists(sess, (live,), n_live, func, ("live",))
-    _place(func, sess, stream, q, out, live, n_live)
+    st = _place(func, sess, stream, q, out, live, n_live)
     _check(getattr(lib(), func)(ctypes.byref(cache), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(q), _ptr(live),
-                                _ptr(n_live), sinks, window, _ptr(out), wp, wn, _stream(stream)), func)
-
-
-def _chunk_tokens(sess: Sessions) -> int:
-    return sum(sess.host[b].qe - sess.host[b].qs for b in range(sess.B))
+                                _ptr(n_live), sinks, window, _ptr(out), wp, wn, st), func)
 
 
 def decode_attend_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
@@ -370,7 +369,7 @@ def attend_chunk(pool: Pool, sess: Sessions, q, live, n_live, out, ws: Workspace
                  stream=None) -> None:
     """The newest qe - qs tokens of each session over a bf16 pool: q, out packed by session, [L][Hq][n][D]."""
     wp, wn = ws.get(workspace_bytes(pool, sess, CALL_CHUNK))
-    _attend("ikv_attend_chunk", pool, sess, q, live, n_live, out, wp, wn, sinks, window, _chunk_tokens(sess), IKV_BF16,
+    _attend("ikv_attend_chunk", pool, sess, q, live, n_live, out, wp, wn, sinks, window, sess.span_tokens, IKV_BF16,
             stream)
 
 
@@ -378,7 +377,7 @@ def attend_chunk_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, w
                        window: int = 0, stream=None) -> None:
     """attend_chunk over the 8-bit cache: q, out of the cache's io_dtype."""
     wp, wn = ws.get(quant_workspace_bytes(cache, sess, CALL_CHUNK))
-    _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, _chunk_tokens(sess),
+    _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, sess.span_tokens,
             cache.io_dtype, stream)
 
 
