@@ -32,14 +32,15 @@ struct AttendArgs {
 };
 
 constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all
-constexpr int FEW_ROUND = 1024;     // workgroups of one resident round of k_attend_few
+constexpr int FEW_WAVES = 8;        // of a workgroup of k_attend_few, at most
+constexpr int CUS = 256;            // a round: one workgroup on each
 constexpr int TILE_KEYS = 64;       // entries per tile of k_attend_tile
 
 struct AttendPlan {
   int max_n;               // longest chunk of the batch
   bool too_large;          // does not fit a launch grid
   bool few;                // every session's rows per KV head fit one 16-row block
-  int heads;               // adjacent KV heads of a workgroup (few)
+  int heads, parts;        // few: adjacent KV heads of a workgroup, waves that share a head's entries
   int splits;              // of the entries of a session
   int blocks;              // row blocks per (session, layer, KV head): one (few)
   int rows;                // rows per block in the split state
@@ -53,37 +54,85 @@ inline int64_t attend_bound(const ikv_session &s, bool decode) {
   return decode ? decode_live_bound(s) : std::max<int64_t>(1, s.N);
 }
 
+// How full n > 0 workgroups leave their rounds of one per CU, in percent.
+inline int64_t attend_fill(int64_t n) { return 100 * n / ((n + CUS - 1) / CUS * CUS); }
+
+// Workgroups of the few-rows kernel: `heads` adjacent KV heads (their rows lie side by side, so
+// together the waves read long pieces) times `parts` waves that share a head's entries and join
+// in LDS, and `splits` of a list over workgroups, joined by a second kernel. Four waves a
+// workgroup; us per call of one-token decodes over int8 rows, 36 layers x 8 KV heads unless
+// stated, (heads, parts, splits):
+//  - the fewest splits that fill a round to 70%, 95% where a wave keeps 4096 entries: one
+//    session of 8192: (4, 1, 3) 105, (4, 1, 7) 110, (4, 1, 14) 117; of 1000: (4, 1, 3) 21,
+//    (4, 1, 7) 24; 48 layers x 92,300 entries: (4, 2, 8) 1483, (4, 2, 10) 1495, (8, 1, 10) 1516.
+//  - lists of uneven bounds (the longest 1.15 times the mean or more): four rounds, so that the
+//    last workgroups are short ones. Five sessions of 2000 to 8000: (4, 2, 3) 354, (4, 1, 3) 369.
+//  - more than a round of long lists: eight waves. 48 x 4 heads, 16 sessions of 517 to 4100:
+//    (4, 2, 1) 480, (4, 1, 1) 507; 16 sessions of 500: (4, 1, 1) 117, (4, 2, 1) 127.
+//  - few heads take fewer adjacent ones and more parts, which cost no second kernel: one layer of
+//    8192: (1, 4, 16) 14.0, (8, 1, 64) 19.6. Lists of up to 512 entries take no splits at all:
+//    300: (2, 2, 1) 11.8, (4, 1, 3) 14.2.
+// A split's state costs rows (D + 2) floats, written and read: lists are cut no finer than 16
+// entries a row, nor for their unevenness finer than 128 (3 tokens of 5 heads in 4 sessions of
+// 700 to 2500: one split 72, four 79, six 87).
+inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t longest, bool uneven) {
+  int widest = 4;
+  while (Hkv % widest) widest /= 2;
+  const int64_t heads_all = groups * Hkv;
+  if (longest <= 512) {
+    p.heads = widest;
+    while (p.heads > 1 && heads_all / p.heads < CUS / 2) p.heads /= 2;
+    p.parts = heads_all < CUS / 2 && longest > 256 ? 8 : 4 / p.heads;
+    p.splits = 1;
+    return;
+  }
+  for (p.heads = widest;; p.heads /= 2) {
+    p.parts = 4 / p.heads;
+    const int64_t units = heads_all / p.heads, finest = std::max(64, 16 * p.rows),
+                  most = std::min<int64_t>(DEC_MAX_SPLITS, longest / (finest * p.parts));
+    p.splits = 0;
+    for (int64_t s = 1; s <= most && !p.splits; ++s)
+      if (attend_fill(units * s) >= (longest / (s * p.parts) >= 4096 ? 95 : 70) && 
+          (!uneven || units * s >= 4 * CUS || longest / (s + 1) < 128 * p.rows))
+        p.splits = int(s);
+    if ((p.splits && p.splits <= 8) || p.heads == 1) {
+      if (!p.splits) p.splits = int(std::max<int64_t>(1, most));
+      if (units * p.splits > CUS && longest / p.splits >= 2048) p.parts *= 2;
+      return;
+    }
+  }
+}
+
 inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int B, bool decode, int sinks, int window) {
   AttendPlan p{};
   const int G = a.Hq / a.Hkv;
-  int64_t longest = 1;
+  int64_t longest = 1, sum = 0;
   for (int b = 0; b < B; ++b) {
     const int n = attend_tokens(sess[b], decode);
     p.max_n = std::max(p.max_n, n);
     int64_t len = attend_bound(sess[b], decode);
     if (window) len = std::min<int64_t>(len, int64_t(sinks) + window + n);
     longest = std::max(longest, len);
+    sum += len;
   }
   p.few = int64_t(p.max_n) * G <= FEW_ROWS;
   p.splits = p.blocks = 1;
+  const int64_t groups = std::max<int64_t>(1, int64_t(a.L) * B);
   if (p.few) {
     p.rows = p.max_n * G;
-    p.heads = a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1;
-    const int64_t wgs = std::max<int64_t>(1, int64_t(a.L) * (a.Hkv / p.heads) * std::max(1, B));
-    int64_t s = std::max<int64_t>(1, FEW_ROUND / wgs);
-    s = std::min<int64_t>(s, (longest + 127) / 128);
-    p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
-  } else if (p.max_n > 0) {
+    attend_few_shape(p, a.Hkv, groups, longest, B > 1 && 20 * longest * B >= 23 * sum);
+  } else {
     const int64_t rows = int64_t(p.max_n) * G;
     p.rows = rows <= 128 ? 128 : 256;
     p.blocks = int(std::min<int64_t>((rows + p.rows - 1) / p.rows, INT32_MAX));
-    const int64_t wgs = int64_t(a.L) * a.Hkv * B * p.blocks;
+    const int64_t wgs = groups * a.Hkv * p.blocks;
     int64_t s = std::max<int64_t>(1, 1024 / wgs);
     s = std::min<int64_t>(s, (longest + 511) / 512);
     p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
   }
-  const int64_t parts = int64_t(B) * a.L * a.Hkv * p.blocks * p.splits * p.rows;
-  if (p.splits > 1) p.ws_floats = parts * (a.D + 2);
+  // the workspace is sized without the window
+  if (window) p.splits = std::min(p.splits, attend_plan(a, sess, B, decode, 0, 0).splits);
+  if (p.splits > 1) p.ws_floats = int64_t(B) * a.L * a.Hkv * p.blocks * p.splits * p.rows * (a.D + 2);
   p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || int64_t(B) * a.L * a.Hkv * p.blocks > (1 << 24);
   return p;
 }

@@ -31,6 +31,8 @@ namespace ikv {
 
 constexpr float FEW_SLACK = 8.f;                 // log2
 constexpr int FEW_BLOCK = 32;                    // entries per block
+typedef uint32_t u32x2_few __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_few __attribute__((ext_vector_type(4)));
 
 // x as bf16 parts, the first the nearest, each next one the nearest of what is left.
 template <int PARTS>
@@ -46,8 +48,9 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_k (&o)[P
   }
 }
 
-template <int FMT, typename IO, int D>
-__global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) {
+template <int FMT, typename IO, int D, bool O32>
+__global__ void __launch_bounds__(64 * FEW_WAVES) __attribute__((amdgpu_waves_per_eu(2)))
+k_attend_few(AttendArgs a, int heads, int rows_max) {
   constexpr int ES = FMT == KV_BF16 ? 2 : 1;     // bytes per element
   constexpr int KS = D / 32;                     // 32-channel steps of the first product
   constexpr int NC = D / 16;                     // channels of a lane in the second
@@ -55,13 +58,15 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
   constexpr int VW = NC * ES / 4;                // words of a lane per value row
   constexpr int QP = sizeof(IO) == 4 ? 3 : 1;    // bf16 parts of the queries
   constexpr int PP = sizeof(IO) == 4 ? 3 : 2;    // and of the weights
-  __shared__ __align__(16) float sc[4][2][FEW_BLOCK];
+  constexpr int NB = 2;                          // blocks of entries in registers (three or four: no faster)
+  __shared__ __align__(16) float sc[FEW_WAVES][2][FEW_BLOCK];
+  extern __shared__ float joint[];               // the parts' states, where a head has several waves
 
-  const int b = blockIdx.z, heads = blockDim.x >> 6;
+  const int b = blockIdx.z;
   const ikv_session s = a.sess[b];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ngrp = a.Hkv / heads;
-  const int l = blockIdx.y / ngrp, hkv = (blockIdx.y - l * ngrp) * heads + w;
+  const int ngrp = a.Hkv / heads, parts_wg = (blockDim.x >> 6) / heads, part_wg = w / heads;
+  const int l = blockIdx.y / ngrp, hkv = (blockIdx.y - l * ngrp) * heads + w % heads;
   const int split = blockIdx.x, nsplit = gridDim.x;
   const int g = lane >> 4, c = lane & 15;
   const int G = a.Hq / a.Hkv;
@@ -80,8 +85,8 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
   const int lo = a.window ? max(0, N - n - a.window + 1) : 0;
   const int first = min(a.sinks, lo), gap = lo - first;        // index v stands for entry v, or v + gap from `first` on
   const int T = N - gap;
-  const int chunk = ((T + nsplit - 1) / nsplit + 15) & ~15;
-  const int v0 = min(T, split * chunk), v1 = min(T, v0 + chunk);
+  const int pieces = nsplit * parts_wg, chunk = ((T + pieces - 1) / pieces + 15) & ~15;
+  const int v0 = min(T, (split * parts_wg + part_wg) * chunk), v1 = min(T, v0 + chunk);
 
   float m = -INFINITY, lsum = 0.f;               // reference of row c; this lane's sum of weights
   f32x4_k o[NC];                                 // o[j][i]: channel NC (4 g + i) + j of row c
@@ -98,10 +103,15 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
       load8(static_cast<const typename std::conditional<sizeof(IO) == 4, float, uint16_t>::type *>(a.q) + q_at + ch, x);
       split_parts<QP>(x, qf[ks]);
     }
-    const int64_t row_bytes = int64_t(a.Hkv) * D * ES;
+    const uint32_t row_bytes = uint32_t(a.Hkv) * D * ES;
     const int64_t layer = int64_t(l) * a.num_slots;
-    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES + 16 * g;
-    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES + c * (NC * ES);
+    // wave-uniform bases; a row is a per-lane byte offset, 32 bits wide where a layer is below 4 GB
+    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES;
+    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES;
+    auto row_at = [&](int sl, uint32_t within) {
+      if constexpr (O32) return uint32_t(sl) * row_bytes + within;
+      else return uint64_t(uint32_t(sl)) * row_bytes + within;
+    };
     const float2 *sbase = reinterpret_cast<const float2 *>(a.scales) + layer * a.Hkv + hkv;
     const int32_t *list = a.live + s.slot_off;
     const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
@@ -117,32 +127,34 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
       return list[v < first ? v : v + gap];
     };
     auto load = [&](Block &x, int sl) __attribute__((always_inline)) {
+      if constexpr (FMT != KV_BF16)                // in the order of use
+        x.s = *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(sbase) + row_at(sl, 0) / (D / 8));
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const char *p = kbase + int64_t(__builtin_amdgcn_ds_bpermute(4 * (16 * kb + c), sl)) * row_bytes;
+        const char *p = kbase + row_at(__builtin_amdgcn_ds_bpermute(4 * (16 * kb + c), sl), 16 * g);
 #pragma unroll
         for (int j = 0; j < KW; ++j) x.k[kb][j] = *reinterpret_cast<const uint4 *>(p + 64 * j);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int at = e < 4 ? 4 * g + e : 16 + 4 * g + e - 4;
-        const char *p = vbase + int64_t(__builtin_amdgcn_ds_bpermute(4 * at, sl)) * row_bytes;
-        if constexpr (VW == 1) x.v[e][0] = *reinterpret_cast<const uint32_t *>(p);
+        const char *p = vbase + row_at(__builtin_amdgcn_ds_bpermute(4 * at, sl), c * (NC * ES));
+        if constexpr (VW == 1) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
         else if constexpr (VW == 2) {
-          const uint2 y = *reinterpret_cast<const uint2 *>(p);
+          const u32x2_few y = __builtin_nontemporal_load(reinterpret_cast<const u32x2_few *>(p));
           x.v[e][0] = y.x;
           x.v[e][1] = y.y;
         } else {
-          const uint4 y = *reinterpret_cast<const uint4 *>(p);
+          const u32x4_few y = __builtin_nontemporal_load(reinterpret_cast<const u32x4_few *>(p));
           x.v[e][0] = y.x;
           x.v[e][1] = y.y;
           x.v[e][2] = y.z;
           x.v[e][3] = y.w;
         }
       }
-      if constexpr (FMT != KV_BF16) x.s = sbase[int64_t(sl) * a.Hkv];
     };
-    auto compute = [&](Block &x, int base, int sl) __attribute__((always_inline)) {
+    bool odd = false;                              // a value that is not finite was left out
+    auto compute = [&](Block &x, int base) __attribute__((always_inline)) {
       f32x4_k acc[2] = {f32x4_k{0.f, 0.f, 0.f, 0.f}, f32x4_k{0.f, 0.f, 0.f, 0.f}};
       if constexpr (FMT != KV_BF16) {
         if (lane < FEW_BLOCK) {
@@ -195,11 +207,9 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int v = base + 16 * kb + 4 * g + i, j = v < first ? v : v + gap;
-            const bool see = v < v1 && j <= own && (a.window == 0 || j < a.sinks || j > own - a.window);
-            if (!see) {
-              hidden |= 1u << (4 * kb + i);
-              acc[kb][i] = -INFINITY;
-            }
+            const bool see = (v < v1) & (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
+            hidden |= see ? 0u : 1u << (4 * kb + i);
+            acc[kb][i] = see ? acc[kb][i] : -INFINITY;
           }
       }
       float tmax = -INFINITY;
@@ -231,27 +241,20 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
           }
           pw[4 * kb + i] = p;
         }
-      // bf16 values that are not finite would turn the zero weights of rows that do not see
-      // them into NaN: such entries are taken out of the product and added row by row
-      uint32_t odd = 0;                            // bit e: this lane's entry e holds one
+      bf16x8_k pf[PP];
+      split_parts<PP>(pw, pf);
       if constexpr (FMT == KV_BF16) {
         if (!whole) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            bool f = false;
+          for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int k = 0; k < VW; ++k) f |= (x.v[e][k] & 0x7f80u) == 0x7f80u || (x.v[e][k] & 0x7f800000u) == 0x7f800000u;
-            if (__builtin_amdgcn_ballot_w64(f) >> (16 * g) & 0xffffu) {
-              odd |= 1u << e;
-#pragma unroll
-              for (int k = 0; k < VW; ++k) x.v[e][k] = 0u;
+            for (int k = 0; k < VW; ++k) {
+              odd |= odd_low(x.v[e][k]) | odd_high(x.v[e][k]);
+              x.v[e][k] = bf16_finite(x.v[e][k]);
             }
-          }
         }
       }
-      bf16x8_k pf[PP];
-      split_parts<PP>(pw, pf);
-      // the operand of channels NC c + j .. + 3 (8-bit) or + 1 (bf16) at a time
+      // the operand of channels NC c + STEP k .. at a time
       constexpr int STEP = FMT == KV_BF16 ? 2 : 4;
 #pragma unroll
       for (int k = 0; k < VW; ++k) {
@@ -276,45 +279,73 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
             o[STEP * k + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[p], o[STEP * k + i], 0, 0, 0);
         }
       }
-      if constexpr (FMT == KV_BF16) {
-        if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+    };
+    // NB blocks in registers: one computed, the others on their way
+    Block x[NB];
+    int sl[NB];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            for (int gg = 0; gg < 4; ++gg) {
-              if (!(__builtin_amdgcn_readlane(odd, 16 * gg) >> e & 1)) continue;
-              const float p = __shfl(pw[e], 16 * gg + c, WAVE);
-              const bool see = !(__shfl(hidden, 16 * gg + c, WAVE) >> e & 1);
-              const int at = e < 4 ? 4 * gg + e : 16 + 4 * gg + e - 4;
-              const uint16_t *row = reinterpret_cast<const uint16_t *>(
-                  static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES +
-                  int64_t(__builtin_amdgcn_readlane(sl, at)) * row_bytes);
+    for (int u = 0; u < NB - 1; ++u) sl[u] = slots(v0 + u * FEW_BLOCK);
+    int next = slots(v0 + (NB - 1) * FEW_BLOCK);
 #pragma unroll
-              for (int j = 0; j < NC; ++j)
+    for (int u = 0; u < NB - 1; ++u) load(x[u], sl[u]);
+    for (int base = v0; base < v1; base += NB * FEW_BLOCK) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (see) o[j][i] = fmaf(p, Store<uint16_t>::ld(row + NC * (4 * g + i) + j), o[j][i]);
+      for (int u = 0; u < NB; ++u) {
+        constexpr int B1 = NB - 1;
+        const int at = base + u * FEW_BLOCK;
+        if (u > 0 && at >= v1) break;
+        __builtin_amdgcn_sched_barrier(0);
+        sl[(u + B1) % NB] = next;
+        next = slots(at + NB * FEW_BLOCK);
+        load(x[(u + B1) % NB], sl[(u + B1) % NB]);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(x[u], at);
+      }
+    }
+    if constexpr (FMT == KV_BF16) {
+      if (__builtin_amdgcn_ballot_w64(odd) != 0)
+        for (int v = v0; v < v1; ++v) {
+          const int e = v < first ? v : v + gap;
+          const bool see = (e <= own) & ((a.window == 0) | (e < a.sinks) | (e > own - a.window));
+          const uint16_t *row = reinterpret_cast<const uint16_t *>(vbase + row_at(list[e], 0));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+              const uint16_t y = row[NC * (4 * g + i) + j];
+              o[j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
             }
         }
-      }
-    };
-    Block A, Bk;
-    int sa = slots(v0), sb = slots(v0 + FEW_BLOCK);
-    load(A, sa);
-    for (int base = v0; base < v1; base += 2 * FEW_BLOCK) {
-      const int s2 = slots(base + 2 * FEW_BLOCK), s3 = slots(base + 3 * FEW_BLOCK);
-      load(Bk, sb);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(A, base, sa);
-      __builtin_amdgcn_sched_barrier(0);
-      load(A, s2);
-      __builtin_amdgcn_sched_barrier(0);
-      if (base + FEW_BLOCK < v1) compute(Bk, base + FEW_BLOCK, sb);
-      sa = s2;
-      sb = s3;
     }
   }
   lsum += __shfl_xor(lsum, 16, WAVE);
   lsum += __shfl_xor(lsum, 32, WAVE);
+  if (parts_wg > 1) {
+    // the other waves of a head leave their state in LDS, lane for lane; the first joins them
+    float *mine = joint + (w - heads) * (4 * NC + 2) * WAVE + lane;
+    if (part_wg > 0) {
+      mine[0] = m;
+      mine[WAVE] = lsum;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(2 + 4 * j + i) * WAVE] = o[j][i];
+    }
+    __syncthreads();
+    if (part_wg > 0) return;
+    for (int p = 1; p < parts_wg; ++p) {
+      const float *x = joint + (w + (p - 1) * heads) * (4 * NC + 2) * WAVE + lane;
+      const float mp = x[0], mn = fmaxf(m, mp);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float fp = mp == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mp - mn);
+      m = mn;
+      lsum = lsum * f + x[WAVE] * fp;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] = o[j][i] * f + x[(2 + 4 * j + i) * WAVE] * fp;
+    }
+  }
   if (c >= rows) return;
   if (nsplit == 1) {
     const float inv = m == -INFINITY ? 0.f : 1.0f / lsum;      // nothing seen: zero
@@ -339,7 +370,12 @@ __global__ void __launch_bounds__(256) k_attend_few(AttendArgs a, int rows_max) 
 template <int FMT, typename IO, int D>
 static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   KTimer kt_("k_attend_few", st);
-  k_attend_few<FMT, IO, D><<<dim3(p.splits, a.L * (a.Hkv / p.heads), a.B), 64 * p.heads, 0, st>>>(a, p.rows);
+  const dim3 grid(unsigned(p.splits), unsigned(a.L * (a.Hkv / p.heads)), unsigned(a.B));
+  const size_t lds = size_t(p.parts - 1) * p.heads * (D / 4 + 2) * WAVE * sizeof(float);
+  if (a.num_slots * a.Hkv * D * (FMT == KV_BF16 ? 2 : 1) < (int64_t(1) << 32))
+    k_attend_few<FMT, IO, D, true><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
+  else
+    k_attend_few<FMT, IO, D, false><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
 }
 
 template <int FMT, typename IO>

@@ -66,7 +66,6 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   __shared__ __align__(16) uint16_t ks_[2][TILE_KEYS * KROW];
   __shared__ __align__(16) uint16_t vs_[2][TILE_KEYS * VROW];
   __shared__ __align__(16) float sc_[2][2][TILE_KEYS];               // scales: keys' (times log2 e / sqrt D), values'
-  __shared__ __align__(16) uint8_t odd_[2][FMT == KV_BF16 ? TILE_KEYS * PPR : 16];   // pieces with a value not finite
 
   // units (session, layer, KV head) in steps of 8, so that a unit's blocks and splits run on
   // one XCD and share its rows in that L2; the blocks with the most entries first
@@ -155,27 +154,19 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       const int ja = va < first ? va : va + gap, jb = vb < first ? vb : vb + gap;
       return !(vb < T && jb <= o0 && (a.window == 0 || jb < a.sinks || ja > o1 - a.window));
     };
+    bool odd = false;                              // a value that is not finite was left out
     auto store = [&](int buf, const Regs &r, int tile) __attribute__((always_inline)) {
       const bool look = FMT == KV_BF16 && edge(tile, own0, own1);
 #pragma unroll
       for (int i = 0; i < PT; ++i) {
         const int p = tid + i * NT, q = p % PIECES, key = q / PPR, at = q % PPR;
-        const bool isv = p >= PIECES;
-        uint16_t *dst = isv ? &vs_[buf][key * VROW] : &ks_[buf][key * KROW];
+        uint16_t *dst = p >= PIECES ? &vs_[buf][key * VROW] : &ks_[buf][key * KROW];
         uint4 x = r.r[i];
         if constexpr (FMT == KV_BF16) {
-          // a value that is not finite would turn the zero weights of rows that do not see it
-          // into NaN: it is left out here and added row by row
-          if (look && isv) {
-            uint32_t u[4] = {x.x, x.y, x.z, x.w};
-            bool odd = false;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if ((u[k] & 0x7f80u) == 0x7f80u) odd = true, u[k] &= 0xffff0000u;
-              if ((u[k] & 0x7f800000u) == 0x7f800000u) odd = true, u[k] &= 0x0000ffffu;
-            }
-            x = make_uint4(u[0], u[1], u[2], u[3]);
-            odd_[buf][q] = odd;
+          if (look && p >= PIECES) {
+            odd |= odd_low(x.x) | odd_high(x.x) | odd_low(x.y) | odd_high(x.y) | odd_low(x.z) | odd_high(x.z) |
+                   odd_low(x.w) | odd_high(x.w);
+            x = make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w));
           }
           *reinterpret_cast<uint4 *>(dst + at * 8) = x;
         } else {
@@ -230,11 +221,9 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int v = va + 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3), j = v < first ? v : v + gap;
-            const bool see = v < T && j <= own && (a.window == 0 || j < a.sinks || j > own - a.window);
-            if (!see) {
-              hidden |= 1u << (16 * kb + i);
-              acc[kb][i] = -INFINITY;
-            }
+            const bool see = (v < T) & (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
+            hidden |= see ? 0u : 1u << (16 * kb + i);
+            acc[kb][i] = see ? acc[kb][i] : -INFINITY;
           }
       }
       float tmax = -INFINITY;
@@ -264,7 +253,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (hidden >> (16 * kb + i) & 1) acc[kb][i] = 0.f;
+            acc[kb][i] = hidden >> (16 * kb + i) & 1 ? 0.f : acc[kb][i];
       }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -287,9 +276,16 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (hidden >> (16 * kb + i) & 1) acc[kb][i] = 0.f;
+              acc[kb][i] = hidden >> (16 * kb + i) & 1 ? 0.f : acc[kb][i];
         }
       }
+      // value operand of 16-entry step st and channels 32 db .. + 31
+      auto values = [&](int st, int db) __attribute__((always_inline)) {
+        const int lr = lane & 15;
+        const uint16_t *vr = &vs_[buf][(16 * st + 4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3) + 32 * db];
+        const uint2 x0 = read_tr16(vr), x1 = read_tr16(vr + 8 * VROW);
+        return make_uint4(x0.x, x0.y, x1.x, x1.y);
+      };
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
         float x[8];
@@ -297,41 +293,11 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         for (int e = 0; e < 8; ++e) x[e] = acc[st >> 1][8 * (st & 1) + e];
         bf16x8_k pf[PP];
         tile_parts<PP>(x, pf);
-        const int lr = lane & 15;
-        const uint16_t *vr = &vs_[buf][(16 * st + 4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3)];
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const uint2 x0 = read_tr16(vr + 32 * db), x1 = read_tr16(vr + 8 * VROW + 32 * db);
-          const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(x0.x, x0.y, x1.x, x1.y));
+          const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, values(st, db));
 #pragma unroll
           for (int p = PP - 1; p >= 0; --p) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[p], o[db], 0, 0, 0);
-        }
-      }
-      if constexpr (FMT == KV_BF16) {
-        if (edge(tile, own0, own1)) {              // the values left out of the tile
-          uint32_t f = 0;
-#pragma unroll
-          for (int k = 0; k < PPR / 4; ++k) f |= reinterpret_cast<const uint32_t *>(&odd_[buf][lane * PPR])[k];
-          uint64_t todo = __builtin_amdgcn_ballot_w64(f != 0);
-          while (todo) {
-            const int key = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const uint16_t *vrow =
-                reinterpret_cast<const uint16_t *>(vbase + int64_t(list[entry(va + key)]) * row_bytes);
-            const int kb = key >> 5, hk = key >> 2 & 1, i = 4 * (key >> 3 & 3) + (key & 3);
-            float p = 0.f;
-#pragma unroll
-            for (int k = 0; k < 32; ++k) p = k == 16 * kb + i ? acc[k >> 4][k & 15] : p;
-            p = __shfl(p, 32 * hk + c, WAVE);
-            const bool see = !(__shfl(hidden, 32 * hk + c, WAVE) >> (16 * kb + i) & 1);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
-                if (see && (y & 0x7f80u) == 0x7f80u) o[db][k] = fmaf(p, Store<uint16_t>::ld(&y), o[db][k]);
-              }
-          }
         }
       }
     };
@@ -358,6 +324,21 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       compute(1, tile + 1);
       store(0, rA, tile + 2);
       __syncthreads();
+    }
+    if constexpr (FMT == KV_BF16) {
+      if (__syncthreads_or(odd))
+        for (int v = tb * TILE_KEYS; v < min(T, te * TILE_KEYS); ++v) {
+          const int j = v < first ? v : v + gap;
+          const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
+          const uint16_t *vrow = reinterpret_cast<const uint16_t *>(vbase + int64_t(list[j]) * row_bytes);
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
+              o[db][k] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+            }
+        }
     }
   }
   lsum += __shfl_xor(lsum, 32, WAVE);

@@ -43,4 +43,13 @@ template <int FMT> __device__ __forceinline__ void codes_across(uint32_t a, uint
   }
 }
 
+// bf16 values that are not finite, by pairs. Zero weights of rows that do not see an entry would
+// turn them into NaN, so where some row does not, the product takes the pair without them, and
+// they are added afterwards to the sums of the rows that do.
+__device__ __forceinline__ bool odd_low(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool odd_high(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t bf16_finite(uint32_t w) {
+  return (odd_low(w) ? 0u : w & 0xffffu) | (odd_high(w) ? 0u : w & 0xffff0000u);
+}
+
 }  // namespace ikv
