@@ -126,16 +126,21 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     const int32_t *list = a.live + s.slot_off;
     const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
 
+    // Staging: in the iteration of tile i, the keys of tile i + 2 and the values and scales of
+    // tile i + 1 go from registers to LDS, and those of the tiles after them are loaded.
     struct Slots { int32_t s[PT], sc; };
     struct Regs { uint4 r[PT]; float2 sc; };
     auto entry = [&](int v) __attribute__((always_inline)) {
-      v = min(v, T - 1);                           // past the end the last one again, masked
+      v = max(0, min(v, T - 1));                   // past the end the last one again, masked
       return v < first ? v : v + gap;
     };
     auto slots = [&](int tile) __attribute__((always_inline)) {
       Slots x;
 #pragma unroll
-      for (int i = 0; i < PT; ++i) x.s[i] = list[entry(tile * TILE_KEYS + (tid + i * NT) % PIECES / PPR)];
+      for (int i = 0; i < PT; ++i) {
+        const int p = tid + i * NT;
+        x.s[i] = list[entry((tile + (p < PIECES ? 1 : 0)) * TILE_KEYS + p % PIECES / PPR)];
+      }
       x.sc = FMT == KV_BF16 ? 0 : list[entry(tile * TILE_KEYS + lane)];
       return x;
     };
@@ -154,13 +159,16 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       const int ja = va < first ? va : va + gap, jb = vb < first ? vb : vb + gap;
       return !(vb < T && jb <= o0 && (a.window == 0 || jb < a.sinks || ja > o1 - a.window));
     };
-    bool odd = false;                              // a value that is not finite was left out
-    auto store = [&](int buf, const Regs &r, int tile) __attribute__((always_inline)) {
-      const bool look = FMT == KV_BF16 && edge(tile, own0, own1);
+    // the values and scales of `tile` (buffer tile & 1) and the keys of tile + 1. A value that is
+    // not finite would turn the zero weights of rows that do not see it into NaN: in a tile that
+    // some row does not see whole it is left out and added after the loop.
+    bool odd = false;
+    auto store = [&](const Regs &r, int tile, int par) __attribute__((always_inline)) {
+      const bool look = edge(tile, own0, own1);
 #pragma unroll
       for (int i = 0; i < PT; ++i) {
         const int p = tid + i * NT, q = p % PIECES, key = q / PPR, at = q % PPR;
-        uint16_t *dst = p >= PIECES ? &vs_[buf][key * VROW] : &ks_[buf][key * KROW];
+        uint16_t *dst = p >= PIECES ? &vs_[par][key * VROW] : &ks_[par ^ 1][key * KROW];
         uint4 x = r.r[i];
         if constexpr (FMT == KV_BF16) {
           if (look && p >= PIECES) {
@@ -177,60 +185,65 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       }
       if constexpr (FMT != KV_BF16) {
         if (tid < TILE_KEYS) {
-          sc_[buf][0][tid] = r.sc.x * to_log2;
-          sc_[buf][1][tid] = r.sc.y;
+          const bool bad = look && !(fabsf(r.sc.y) < INFINITY);
+          odd |= bad;
+          sc_[par][0][tid] = r.sc.x * to_log2;
+          sc_[par][1][tid] = bad ? 0.f : r.sc.y;
         }
       }
     };
-    auto compute = [&](int buf, int tile) __attribute__((always_inline)) {
-      // nothing of the tile for this wave: past its newest token, or before its window and after the sinks
-      const int va = tile * TILE_KEYS, vb = va + TILE_KEYS - 1;
-      const int ja = va < first ? va : va + gap, jb = vb < first ? vb : vb + gap;
-      if (!wave_on || ja > wown1 || (a.window && ja >= a.sinks && jb <= wown0 - a.window)) return;
-      f32x16_k acc[2];
+    typedef f32x16_k Logits[2];
+    // channels 16 ks of the logits of a tile whose keys are in buffer `par`, both 32-entry halves
+    auto first_product = [&](Logits &x, int par, int ks) __attribute__((always_inline)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
+        const bf16x8_k kf = *reinterpret_cast<const bf16x8_k *>(&ks_[par][(32 * kb + c) * KROW + 8 * h2 + 16 * ks]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[kb][i] = 0.f;
-        const uint16_t *kr = &ks_[buf][(32 * kb + c) * KROW + 8 * h2];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const bf16x8_k kf = *reinterpret_cast<const bf16x8_k *>(kr + 16 * ks);
-#pragma unroll
-          for (int p = QP - 1; p >= 0; --p)
-            acc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][p], acc[kb], 0, 0, 0);
-        }
+        for (int p = QP - 1; p >= 0; --p) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][p], x[kb], 0, 0, 0);
       }
+    };
+    auto second_product = [&](const bf16x8_k (&pf)[PP], int par, int st) __attribute__((always_inline)) {
+      const int lr = lane & 15;
+      const uint16_t *vr = &vs_[par][(16 * st + 4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3)];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int db = 0; db < DB; ++db) {
+        const uint2 x0 = read_tr16(vr + 32 * db), x1 = read_tr16(vr + 8 * VROW + 32 * db);
+        const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(x0.x, x0.y, x1.x, x1.y));
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          if constexpr (FMT != KV_BF16) {
-            const float4 ks = *reinterpret_cast<const float4 *>(&sc_[buf][0][32 * kb + 8 * i4 + 4 * h2]);
-            acc[kb][4 * i4] *= ks.x;
-            acc[kb][4 * i4 + 1] *= ks.y;
-            acc[kb][4 * i4 + 2] *= ks.z;
-            acc[kb][4 * i4 + 3] *= ks.w;
+        for (int p = PP - 1; p >= 0; --p) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[p], o[db], 0, 0, 0);
+      }
+    };
+    // The iteration of `tile`, its logits in x (raw products): their scales, mask and reference,
+    // then its weights and second product beside the first product of the next tile (into y).
+    auto step = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Slots &sl) __attribute__((always_inline)) {
+      if constexpr (FMT != KV_BF16) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const float4 ks = *reinterpret_cast<const float4 *>(&sc_[par][0][32 * kb + 8 * i4 + 4 * h2]);
+            x[kb][4 * i4] *= ks.x;
+            x[kb][4 * i4 + 1] *= ks.y;
+            x[kb][4 * i4 + 2] *= ks.z;
+            x[kb][4 * i4 + 3] *= ks.w;
           }
-        }
-      const bool part = edge(tile, wown0, wown1);
-      uint32_t hidden = 0;                         // bit 16 kb + i: not seen by this lane's row
-      if (part) {
+      }
+      if (edge(tile, wown0, wown1)) {
+        const int va = tile * TILE_KEYS;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int v = va + 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3), j = v < first ? v : v + gap;
             const bool see = (v < T) & (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
-            hidden |= see ? 0u : 1u << (16 * kb + i);
-            acc[kb][i] = see ? acc[kb][i] : -INFINITY;
+            x[kb][i] = see ? x[kb][i] : -INFINITY;
           }
       }
       float tmax = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, acc[kb][i]);
+        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, x[kb][i]);
       if constexpr (FMT == KV_BF16) tmax *= to_log2;
       if (__builtin_amdgcn_ballot_w64(!(tmax - m <= TILE_SLACK)) != 0) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
@@ -241,95 +254,78 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] *= corr;
       }
+      const float ms = m == -INFINITY ? 0.f : m;   // a row that has seen nothing: its weights are 2^-inf
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[kb][i] = 0.f;
+      store(r, tile + 1, par ^ 1);
+      load(sl, r);
       float sum = 0.f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          acc[kb][i] = __builtin_amdgcn_exp2f(FMT == KV_BF16 ? fmaf(acc[kb][i], to_log2, -m) : acc[kb][i] - m);
-        }
-      if (part) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            acc[kb][i] = hidden >> (16 * kb + i) & 1 ? 0.f : acc[kb][i];
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum += acc[kb][i];
-      lsum += sum;
-      if constexpr (FMT != KV_BF16) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) {
-            const float4 vs = *reinterpret_cast<const float4 *>(&sc_[buf][1][32 * kb + 8 * i4 + 4 * h2]);
-            acc[kb][4 * i4] *= vs.x;
-            acc[kb][4 * i4 + 1] *= vs.y;
-            acc[kb][4 * i4 + 2] *= vs.z;
-            acc[kb][4 * i4 + 3] *= vs.w;
-          }
-        if (part) {                                // the scale of an unseen row may be anything
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              acc[kb][i] = hidden >> (16 * kb + i) & 1 ? 0.f : acc[kb][i];
-        }
-      }
-      // value operand of 16-entry step st and channels 32 db .. + 31
-      auto values = [&](int st, int db) __attribute__((always_inline)) {
-        const int lr = lane & 15;
-        const uint16_t *vr = &vs_[buf][(16 * st + 4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3) + 32 * db];
-        const uint2 x0 = read_tr16(vr), x1 = read_tr16(vr + 8 * VROW);
-        return make_uint4(x0.x, x0.y, x1.x, x1.y);
-      };
-#pragma unroll
       for (int st = 0; st < 4; ++st) {
-        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = acc[st >> 1][8 * (st & 1) + e];
-        bf16x8_k pf[PP];
-        tile_parts<PP>(x, pf);
+        for (int ks = st * KS / 4; ks < (st + 1) * KS / 4; ++ks) first_product(y, par ^ 1, ks);
+        float w[8];
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, values(st, db));
-#pragma unroll
-          for (int p = PP - 1; p >= 0; --p) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[p], o[db], 0, 0, 0);
+        for (int e = 0; e < 8; ++e) {
+          const float z = x[st >> 1][8 * (st & 1) + e];
+          w[e] = __builtin_amdgcn_exp2f(FMT == KV_BF16 ? fmaf(z, to_log2, -ms) : z - ms);
+          sum += w[e];
         }
+        if constexpr (FMT != KV_BF16) {
+#pragma unroll
+          for (int i4 = 0; i4 < 2; ++i4) {
+            const float4 vs = *reinterpret_cast<const float4 *>(&sc_[par][1][16 * st + 8 * i4 + 4 * h2]);
+            w[4 * i4] *= vs.x;
+            w[4 * i4 + 1] *= vs.y;
+            w[4 * i4 + 2] *= vs.z;
+            w[4 * i4 + 3] *= vs.w;
+          }
+        }
+        bf16x8_k pf[PP];
+        tile_parts<PP>(w, pf);
+        second_product(pf, par, st);
+      }
+      lsum += sum;
+    };
+    auto iterate = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Slots &sl) __attribute__((always_inline)) {
+      if (wave_on) step(x, y, tile, par, r, sl);
+      else {
+        store(r, tile + 1, par ^ 1);
+        load(sl, r);
       }
     };
-    Regs rA, rB;
-    load(slots(tb), rA);
-    Slots s1 = slots(tb + 1);
-    __builtin_amdgcn_sched_barrier(0);
-    load(s1, rB);
-    store(0, rA, tb);
-    Slots s2 = slots(tb + 2);
+    Logits sA, sB;
+    Regs r;
+    load(slots(tb - 1), r);                        // keys of the first tile (and values of the one before: the list's
+    store(r, tb - 1, 1);                           // first again, overwritten)
+    load(slots(tb), r);
+    store(r, tb, 0);
+    load(slots(tb + 1), r);
+    Slots sl = slots(tb + 2);
     __syncthreads();
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sA[kb][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) first_product(sA, 0, ks);
+    __syncthreads();                               // before keys of tile tb + 2 take that buffer
     for (int tile = tb; tile < te; tile += 2) {
-      // buffer 0 holds `tile`, rB tile + 1
-      const Slots s3 = slots(tile + 3);
-      load(s2, rA);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(0, tile);
-      store(1, rB, tile + 1);
+      Slots s2 = slots(tile + 3);
+      iterate(sA, sB, tile, 0, r, sl);
       __syncthreads();
       if (tile + 1 >= te) break;
-      s2 = slots(tile + 4);
-      load(s3, rB);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(1, tile + 1);
-      store(0, rA, tile + 2);
+      sl = slots(tile + 4);
+      iterate(sB, sA, tile + 1, 1, r, s2);
       __syncthreads();
     }
-    if constexpr (FMT == KV_BF16) {
-      if (__syncthreads_or(odd))
-        for (int v = tb * TILE_KEYS; v < min(T, te * TILE_KEYS); ++v) {
-          const int j = v < first ? v : v + gap;
-          const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
+    if (__syncthreads_or(odd))
+      for (int v = tb * TILE_KEYS; v < min(T, te * TILE_KEYS); ++v) {
+        const int j = v < first ? v : v + gap;
+        const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
+        if constexpr (FMT == KV_BF16) {
           const uint16_t *vrow = reinterpret_cast<const uint16_t *>(vbase + int64_t(list[j]) * row_bytes);
 #pragma unroll
           for (int db = 0; db < DB; ++db)
@@ -338,8 +334,13 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
               const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
               o[db][k] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
             }
+        } else {
+          const float vs = sbase[int64_t(list[j]) * a.Hkv].y;
+          const float add = see && !(fabsf(vs) < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db] += add;
         }
-    }
+      }
   }
   lsum += __shfl_xor(lsum, 32, WAVE);
   if (row >= rows) return;
