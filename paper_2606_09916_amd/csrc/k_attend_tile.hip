@@ -51,7 +51,7 @@ __device__ __forceinline__ void tile_parts(const float *x, bf16x8_k (&o)[PARTS])
   }
 }
 
-template <int FMT, typename IO, int D, int NW>
+template <int FMT, typename IO, int D, int NW, bool O32>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   constexpr int ES = FMT == KV_BF16 ? 2 : 1;
@@ -60,9 +60,9 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   constexpr int KROW = D + 8, VROW = D + 32;
   constexpr int PPR = D * ES / 16;               // 16-byte pieces of a row
   constexpr int PIECES = TILE_KEYS * PPR;        // of a tile's keys (as many of its values)
-  constexpr int PT = 2 * PIECES / NT;            // pieces of a thread: keys first, then values
+  constexpr int PP_ = PIECES > NT ? PIECES / NT : 1;       // pieces of keys, and of values, of a thread
   constexpr int QP = sizeof(IO) == 4 ? 3 : 1, PP = QP;
-  static_assert(2 * PIECES % NT == 0 && (PIECES % NT == 0 || NT % PIECES == 0), "whole pieces");
+  static_assert(PIECES % NT == 0 || 2 * PIECES == NT, "whole pieces, or one of keys or values a thread");
   __shared__ __align__(16) uint16_t ks_[2][TILE_KEYS * KROW];
   __shared__ __align__(16) uint16_t vs_[2][TILE_KEYS * VROW];
   __shared__ __align__(16) float sc_[2][2][TILE_KEYS];               // scales: keys' (times log2 e / sqrt D), values'
@@ -118,7 +118,12 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
                 8 * h2, x);
       tile_parts<QP>(x, qf[ks]);
     }
-    const int64_t row_bytes = int64_t(a.Hkv) * D * ES;
+    const uint32_t row_bytes = uint32_t(a.Hkv) * D * ES;
+    // byte offset of a slot's row: 32 bits, by a 24-bit product, where slots, rows and layers are small enough
+    auto row_at = [&](int sl) __attribute__((always_inline)) {
+      if constexpr (O32) return uint32_t(__umul24(uint32_t(sl), row_bytes));
+      else return uint64_t(uint32_t(sl)) * row_bytes;
+    };
     const int64_t layer = int64_t(l) * a.num_slots;
     const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES;
     const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES;
@@ -127,31 +132,63 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
 
     // Staging: in the iteration of tile i, the keys of tile i + 2 and the values and scales of
-    // tile i + 1 go from registers to LDS, and those of the tiles after them are loaded.
-    struct Slots { int32_t s[PT], sc; };
-    struct Regs { uint4 r[PT]; float2 sc; };
+    // tile i + 1 go from registers to LDS, and those of the tiles after them are loaded. A
+    // thread's pieces of a tile's values lie in the rows of its pieces of the keys, an iteration
+    // later: a row's byte offset is found once. Tiles wholly past the sinks and before the end
+    // read their slots at a uniform address.
+    const bool takes_k = PIECES >= NT || tid < PIECES, takes_v = PIECES >= NT || tid >= PIECES;
+    typedef typename std::conditional<O32, uint32_t, uint64_t>::type Off;
+    struct Regs {
+      uint4 k[PP_], v[PP_];
+      float2 sc;                                   // int8: of entry `lane`
+      float ks[PP_], vs[PP_];                      // E4M3: of the pieces' rows
+    };
+    struct Slots { int32_t s[PP_], sc; };
+    struct Offs { Off o[PP_], sc; };
     auto entry = [&](int v) __attribute__((always_inline)) {
       v = max(0, min(v, T - 1));                   // past the end the last one again, masked
       return v < first ? v : v + gap;
     };
+    const int key0 = tid % PIECES / PPR;           // of the thread's first piece; each next one NT / PPR on
     auto slots = [&](int tile) __attribute__((always_inline)) {
       Slots x;
+      const int va = tile * TILE_KEYS;
+      if (va >= first && va + TILE_KEYS <= T) {
+        const int32_t *at = list + (va + gap);
 #pragma unroll
-      for (int i = 0; i < PT; ++i) {
-        const int p = tid + i * NT;
-        x.s[i] = list[entry((tile + (p < PIECES ? 1 : 0)) * TILE_KEYS + p % PIECES / PPR)];
+        for (int i = 0; i < PP_; ++i) x.s[i] = at[key0 + i * (NT / PPR)];
+        if constexpr (FMT == KV_INT8) x.sc = at[lane];
+      } else {
+#pragma unroll
+        for (int i = 0; i < PP_; ++i) x.s[i] = list[entry(va + key0 + i * (NT / PPR))];
+        if constexpr (FMT == KV_INT8) x.sc = list[entry(va + lane)];
       }
-      x.sc = FMT == KV_BF16 ? 0 : list[entry(tile * TILE_KEYS + lane)];
       return x;
     };
-    auto load = [&](const Slots &x, Regs &r) __attribute__((always_inline)) {
+    auto offsets = [&](const Slots &x) __attribute__((always_inline)) {
+      Offs y;
 #pragma unroll
-      for (int i = 0; i < PT; ++i) {
-        const int p = tid + i * NT;
-        r.r[i] = *reinterpret_cast<const uint4 *>((p < PIECES ? kbase : vbase) + int64_t(x.s[i]) * row_bytes +
-                                                  p % PPR * 16);
+      for (int i = 0; i < PP_; ++i) y.o[i] = row_at(x.s[i]) + Off(tid % PPR * 16);
+      if constexpr (FMT == KV_INT8) y.sc = row_at(x.sc);
+      return y;
+    };
+    auto scale_at = [&](Off row) __attribute__((always_inline)) {           // of a row offset: 8 bytes for D
+      return *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(sbase) + (row / D) * 8);
+    };
+    // the keys of one tile (offsets k) and the values and scales of the one before (offsets v)
+    auto load = [&](const Offs &k, const Offs &v, Regs &r) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < PP_; ++i) {
+        if (takes_k) {
+          r.k[i] = *reinterpret_cast<const uint4 *>(kbase + k.o[i]);
+          if constexpr (FMT == KV_E4M3) r.ks[i] = scale_at(k.o[i]).x;
+        }
+        if (takes_v) {
+          r.v[i] = *reinterpret_cast<const uint4 *>(vbase + v.o[i]);
+          if constexpr (FMT == KV_E4M3) r.vs[i] = scale_at(v.o[i]).y;
+        }
       }
-      if constexpr (FMT != KV_BF16) r.sc = sbase[int64_t(x.sc) * a.Hkv];
+      if constexpr (FMT == KV_INT8) r.sc = scale_at(v.sc);
     };
     // whether some token of [o0, o1] does not see all of the tile's entries
     auto edge = [&](int tile, int o0, int o1) __attribute__((always_inline)) {
@@ -163,29 +200,44 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     // not finite would turn the zero weights of rows that do not see it into NaN: in a tile that
     // some row does not see whole it is left out and added after the loop.
     bool odd = false;
+    auto put = [&](uint16_t *dst, uint4 x, float scale, bool look) __attribute__((always_inline)) {
+      if constexpr (FMT == KV_BF16) {
+        if (look) {
+          odd |= odd_low(x.x) | odd_high(x.x) | odd_low(x.y) | odd_high(x.y) | odd_low(x.z) | odd_high(x.z) |
+                 odd_low(x.w) | odd_high(x.w);
+          x = make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w));
+        }
+        *reinterpret_cast<uint4 *>(dst) = x;
+      } else {
+        uint2 y[4];
+        if constexpr (FMT == KV_E4M3) {
+          y[0] = e4m3_scaled4(x.x, scale), y[1] = e4m3_scaled4(x.y, scale);
+          y[2] = e4m3_scaled4(x.z, scale), y[3] = e4m3_scaled4(x.w, scale);
+          const bool bad = !(scale < INFINITY);
+          if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) {
+            odd |= look;
+            y[0] = y[1] = y[2] = y[3] = look ? make_uint2(0u, 0u) : make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+          }
+        } else {
+          y[0] = codes4<FMT>(x.x), y[1] = codes4<FMT>(x.y), y[2] = codes4<FMT>(x.z), y[3] = codes4<FMT>(x.w);
+        }
+        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(y[0].x, y[0].y, y[1].x, y[1].y);
+        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(y[2].x, y[2].y, y[3].x, y[3].y);
+      }
+    };
     auto store = [&](const Regs &r, int tile, int par) __attribute__((always_inline)) {
       const bool look = edge(tile, own0, own1);
+      constexpr int EL = 16 / ES;                  // elements of a piece
+      const int at = tid % PPR * EL;
 #pragma unroll
-      for (int i = 0; i < PT; ++i) {
-        const int p = tid + i * NT, q = p % PIECES, key = q / PPR, at = q % PPR;
-        uint16_t *dst = p >= PIECES ? &vs_[par][key * VROW] : &ks_[par ^ 1][key * KROW];
-        uint4 x = r.r[i];
-        if constexpr (FMT == KV_BF16) {
-          if (look && p >= PIECES) {
-            odd |= odd_low(x.x) | odd_high(x.x) | odd_low(x.y) | odd_high(x.y) | odd_low(x.z) | odd_high(x.z) |
-                   odd_low(x.w) | odd_high(x.w);
-            x = make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w));
-          }
-          *reinterpret_cast<uint4 *>(dst + at * 8) = x;
-        } else {
-          const uint2 p0 = codes4<FMT>(x.x), p1 = codes4<FMT>(x.y), p2 = codes4<FMT>(x.z), p3 = codes4<FMT>(x.w);
-          *reinterpret_cast<uint4 *>(dst + at * 16) = make_uint4(p0.x, p0.y, p1.x, p1.y);
-          *reinterpret_cast<uint4 *>(dst + at * 16 + 8) = make_uint4(p2.x, p2.y, p3.x, p3.y);
-        }
+      for (int i = 0; i < PP_; ++i) {
+        const int key = key0 + i * (NT / PPR);
+        if (takes_k) put(&ks_[par ^ 1][key * KROW + at], r.k[i], r.ks[i], false);
+        if (takes_v) put(&vs_[par][key * VROW + at], r.v[i], r.vs[i], look);
       }
-      if constexpr (FMT != KV_BF16) {
+      if constexpr (FMT == KV_INT8) {
         if (tid < TILE_KEYS) {
-          const bool bad = look && !(fabsf(r.sc.y) < INFINITY);
+          const bool bad = look && !(r.sc.y < INFINITY);
           odd |= bad;
           sc_[par][0][tid] = r.sc.x * to_log2;
           sc_[par][1][tid] = bad ? 0.f : r.sc.y;
@@ -215,8 +267,8 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     };
     // The iteration of `tile`, its logits in x (raw products): their scales, mask and reference,
     // then its weights and second product beside the first product of the next tile (into y).
-    auto step = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Slots &sl) __attribute__((always_inline)) {
-      if constexpr (FMT != KV_BF16) {
+    auto step = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Offs &ko, const Offs &vo) __attribute__((always_inline)) {
+      if constexpr (FMT == KV_INT8) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -244,7 +296,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, x[kb][i]);
-      if constexpr (FMT == KV_BF16) tmax *= to_log2;
+      if constexpr (FMT != KV_INT8) tmax *= to_log2;
       if (__builtin_amdgcn_ballot_w64(!(tmax - m <= TILE_SLACK)) != 0) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
         const float mn = fmaxf(m, tmax);
@@ -260,7 +312,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[kb][i] = 0.f;
       store(r, tile + 1, par ^ 1);
-      load(sl, r);
+      load(ko, vo, r);
       float sum = 0.f;
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
@@ -270,10 +322,10 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float z = x[st >> 1][8 * (st & 1) + e];
-          w[e] = __builtin_amdgcn_exp2f(FMT == KV_BF16 ? fmaf(z, to_log2, -ms) : z - ms);
+          w[e] = __builtin_amdgcn_exp2f(FMT == KV_INT8 ? z - ms : fmaf(z, to_log2, -ms));
           sum += w[e];
         }
-        if constexpr (FMT != KV_BF16) {
+        if constexpr (FMT == KV_INT8) {
 #pragma unroll
           for (int i4 = 0; i4 < 2; ++i4) {
             const float4 vs = *reinterpret_cast<const float4 *>(&sc_[par][1][16 * st + 8 * i4 + 4 * h2]);
@@ -289,21 +341,24 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       }
       lsum += sum;
     };
-    auto iterate = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Slots &sl) __attribute__((always_inline)) {
-      if (wave_on) step(x, y, tile, par, r, sl);
+    auto iterate = [&](Logits &x, Logits &y, int tile, int par, Regs &r, const Offs &ko, const Offs &vo)
+        __attribute__((always_inline)) {
+      if (wave_on) step(x, y, tile, par, r, ko, vo);
       else {
         store(r, tile + 1, par ^ 1);
-        load(sl, r);
+        load(ko, vo, r);
       }
     };
     Logits sA, sB;
     Regs r;
-    load(slots(tb - 1), r);                        // keys of the first tile (and values of the one before: the list's
-    store(r, tb - 1, 1);                           // first again, overwritten)
-    load(slots(tb), r);
+    Offs oa = offsets(slots(tb)), ob = offsets(slots(tb + 1));
+    load(oa, oa, r);
+    store(r, tb - 1, 1);                           // keys of the first tile (its values too, overwritten below)
+    load(ob, oa, r);
     store(r, tb, 0);
-    load(slots(tb + 1), r);
-    Slots sl = slots(tb + 2);
+    oa = offsets(slots(tb + 2));
+    load(oa, ob, r);
+    Slots next = slots(tb + 3);
     __syncthreads();
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -313,12 +368,14 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     for (int ks = 0; ks < KS; ++ks) first_product(sA, 0, ks);
     __syncthreads();                               // before keys of tile tb + 2 take that buffer
     for (int tile = tb; tile < te; tile += 2) {
-      Slots s2 = slots(tile + 3);
-      iterate(sA, sB, tile, 0, r, sl);
+      ob = offsets(next);                          // of tile + 3; oa are those of tile + 2
+      next = slots(tile + 4);
+      iterate(sA, sB, tile, 0, r, ob, oa);
       __syncthreads();
       if (tile + 1 >= te) break;
-      sl = slots(tile + 4);
-      iterate(sB, sA, tile + 1, 1, r, s2);
+      oa = offsets(next);
+      next = slots(tile + 5);
+      iterate(sB, sA, tile + 1, 1, r, oa, ob);
       __syncthreads();
     }
     if (__syncthreads_or(odd))
@@ -326,7 +383,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         const int j = v < first ? v : v + gap;
         const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
         if constexpr (FMT == KV_BF16) {
-          const uint16_t *vrow = reinterpret_cast<const uint16_t *>(vbase + int64_t(list[j]) * row_bytes);
+          const uint16_t *vrow = reinterpret_cast<const uint16_t *>(vbase + row_at(list[j]));
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -335,8 +392,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
               o[db][k] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
             }
         } else {
-          const float vs = sbase[int64_t(list[j]) * a.Hkv].y;
-          const float add = see && !(fabsf(vs) < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;
+          const float add = see && !(scale_at(row_at(list[j])).y < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;
 #pragma unroll
           for (int db = 0; db < DB; ++db) o[db] += add;
         }
@@ -380,8 +436,12 @@ template <int FMT, typename IO, int D, int NW>
 static void go_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   const int units = a.B * a.L * a.Hkv;
   KTimer kt_("k_attend_tile", st);
-  k_attend_tile<FMT, IO, D, NW><<<dim3(unsigned((units + 7) / 8 * 8 * p.blocks * p.splits)), 64 * NW, 0, st>>>(
-      a, p.blocks, p.splits, units);
+  const dim3 grid(unsigned((units + 7) / 8 * 8 * p.blocks * p.splits));
+  const int64_t row = int64_t(a.Hkv) * D * (FMT == KV_BF16 ? 2 : 1);
+  if (a.num_slots <= (1 << 24) && row < (1 << 24) && a.num_slots * row <= (int64_t(1) << 32))
+    k_attend_tile<FMT, IO, D, NW, true><<<grid, 64 * NW, 0, st>>>(a, p.blocks, p.splits, units);
+  else
+    k_attend_tile<FMT, IO, D, NW, false><<<grid, 64 * NW, 0, st>>>(a, p.blocks, p.splits, units);
 }
 
 template <int FMT, typename IO>

@@ -22,6 +22,12 @@ template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
 
+// 4 adjacent E4M3 codes of a word times a power of two -> 4 bf16, exactly.
+__device__ __forceinline__ uint2 e4m3_scaled4(uint32_t w, float scale) {
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
+}
+
 // 4 adjacent codes of a word -> 4 bf16.
 template <int FMT> __device__ __forceinline__ uint2 codes4(uint32_t w) {
   if constexpr (FMT == KV_E4M3) return make_uint2(e4m3_pair<false>(w), e4m3_pair<true>(w));
