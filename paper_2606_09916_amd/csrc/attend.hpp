@@ -31,7 +31,8 @@ struct AttendArgs {
   float *ws;
 };
 
-constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all
+constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all (twice that
+                                    // over the 8-bit cache with bf16 outputs)
 constexpr int FEW_WAVES = 8;        // of a workgroup of k_attend_few, at most
 constexpr int CUS = 256;            // a round: one workgroup on each
 constexpr int TILE_KEYS = 64;       // entries per tile of k_attend_tile
@@ -82,7 +83,7 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
   if (longest <= 512) {
     p.heads = widest;
     while (p.heads > 1 && heads_all / p.heads < CUS / 2) p.heads /= 2;
-    p.parts = heads_all < CUS / 2 && longest > 256 ? 8 : 4 / p.heads;
+    p.parts = heads_all < CUS / 2 && longest > 256 && p.rows <= FEW_ROWS ? 8 : 4 / p.heads;
     p.splits = 1;
     return;
   }
@@ -97,10 +98,29 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
         p.splits = int(s);
     if ((p.splits && p.splits <= 8) || p.heads == 1) {
       if (!p.splits) p.splits = int(std::max<int64_t>(1, most));
-      if (units * p.splits > CUS && longest / p.splits >= 2048) p.parts *= 2;
+      if (units * p.splits > CUS && longest / p.splits >= 2048 && p.rows <= FEW_ROWS) p.parts *= 2;
       return;
     }
   }
+}
+
+// Splits of the tile kernel, whose state is up to 256 rows of a split and worth only idle CUs
+// (us, Qwen3-8B's heads, n new tokens over 8701 int8 entries):
+//  - less than a round of workgroups: as many splits as fill one, of at least 256 entries. One
+//    layer, n = 509: 1 split 275, 4 111, 8 120; n = 64: 1 275, 24 36, 48 49.
+//  - one block of rows per head (mostly reading, and the state is small): of at least 1024
+//    entries, five rounds for 128 rows (36 layers, n = 20: 333 with one split, 275 with three, 265
+//    with five, 270 with eight), or the fewest that fill their rounds to 80% for 256 (n = 64: 616
+//    with one, 553 with two, 527 with three, 545 with five).
+//  - else none: n = 128: 903 with one, 944 with two.
+inline int attend_tile_splits(int64_t wgs, int rows, int blocks, int64_t longest) {
+  if (wgs < CUS) return int(std::max<int64_t>(1, std::min<int64_t>({CUS / wgs, longest / 256, DEC_MAX_SPLITS})));
+  if (blocks > 1) return 1;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(5, longest / 1024));
+  if (rows == 128) return int(std::min<int64_t>(most, (5 * CUS + wgs - 1) / wgs));
+  int64_t s = 1;
+  while (s < most && attend_fill(wgs * s) < 80) ++s;
+  return int(s);
 }
 
 inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int B, bool decode, int sinks, int window) {
@@ -115,7 +135,7 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     longest = std::max(longest, len);
     sum += len;
   }
-  p.few = int64_t(p.max_n) * G <= FEW_ROWS;
+  p.few = int64_t(p.max_n) * G <= (a.format != KV_BF16 && !a.io_f32 ? 2 * FEW_ROWS : FEW_ROWS);
   p.splits = p.blocks = 1;
   const int64_t groups = std::max<int64_t>(1, int64_t(a.L) * B);
   if (p.few) {
@@ -123,12 +143,9 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     attend_few_shape(p, a.Hkv, groups, longest, B > 1 && 20 * longest * B >= 23 * sum);
   } else {
     const int64_t rows = int64_t(p.max_n) * G;
-    p.rows = rows <= 128 ? 128 : 256;
+    p.rows = rows <= 128 ? 128 : 256;            // four waves or eight
     p.blocks = int(std::min<int64_t>((rows + p.rows - 1) / p.rows, INT32_MAX));
-    const int64_t wgs = groups * a.Hkv * p.blocks;
-    int64_t s = std::max<int64_t>(1, 1024 / wgs);
-    s = std::min<int64_t>(s, (longest + 511) / 512);
-    p.splits = int(std::min<int64_t>(s, DEC_MAX_SPLITS));
+    p.splits = attend_tile_splits(groups * a.Hkv * p.blocks, p.rows, p.blocks, longest);
   }
   // the workspace is sized without the window
   if (window) p.splits = std::min(p.splits, attend_plan(a, sess, B, decode, 0, 0).splits);

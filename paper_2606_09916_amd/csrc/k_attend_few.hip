@@ -1,5 +1,6 @@
 // Attention of few query rows: the decode of one token, or a chunk of a few tokens whose
-// rows (n tokens x Hq / Hkv heads) of a KV head fit one 16-row matrix block.
+// rows (n tokens x Hq / Hkv heads) of a KV head fit one 16-row matrix block, or two (NR) over
+// the 8-bit cache with bf16 outputs (the other types' registers hold one).
 //
 // Bound by reading the rows of the list once (2 D + 8 bytes per entry, head and layer in
 // 8-bit form, 4 D in bf16). A wave owns one KV head and a split of the list and keeps
@@ -20,8 +21,6 @@
 // float32 ones, and three for float32 queries: 2^-25), which costs matrix work that the
 // reads hide.
 #include <math.h>
-
-#include <type_traits>
 
 #include "attend.hpp"
 #include "ikv_internal.hpp"
@@ -48,7 +47,7 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_k (&o)[P
   }
 }
 
-template <int FMT, typename IO, int D, bool O32>
+template <int FMT, typename IO, int D, int NR, bool O32>
 __global__ void __launch_bounds__(64 * FEW_WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 k_attend_few(AttendArgs a, int heads, int rows_max) {
   constexpr int ES = FMT == KV_BF16 ? 2 : 1;     // bytes per element
@@ -76,33 +75,47 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
   if (a.decode) before = b;
   else
     for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
-  // row r: token r / G, head r % G of the group; rows past the last repeat it and are not written
-  const int r = min(c, rows - 1), t = r / G, h = r - t * G;
-  const int64_t q_at = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D;
+  // row r = 16 k + c of this lane: token r / G, head r % G of the group; rows past the last repeat
+  // it and are not written
+  const int N = max(0, min(a.n_live[b], s.N));
+  int own[NR];                                   // list entry of the row's token
+  int64_t q_at[NR];
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    const int r = min(16 * k + c, rows - 1), t = r / G, h = r - t * G;
+    own[k] = N - n + t;
+    q_at[k] = before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D;
+  }
 
-  // entries seen by any token: the first `skip` ... no more than the sinks, then [lo, N)
-  const int N = max(0, min(a.n_live[b], s.N)), own = N - n + t;
+  // entries seen by any token: up to the sinks, then [lo, N)
   const int lo = a.window ? max(0, N - n - a.window + 1) : 0;
   const int first = min(a.sinks, lo), gap = lo - first;        // index v stands for entry v, or v + gap from `first` on
   const int T = N - gap;
   const int pieces = nsplit * parts_wg, chunk = ((T + pieces - 1) / pieces + 15) & ~15;
   const int v0 = min(T, (split * parts_wg + part_wg) * chunk), v1 = min(T, v0 + chunk);
 
-  float m = -INFINITY, lsum = 0.f;               // reference of row c; this lane's sum of weights
-  f32x4_k o[NC];                                 // o[j][i]: channel NC (4 g + i) + j of row c
+  float m[NR], lsum[NR];                         // reference of row 16 k + c; this lane's sum of its weights
+  f32x4_k o[NR][NC];                             // o[k][j][i]: channel NC (4 g + i) + j of that row
 #pragma unroll
-  for (int j = 0; j < NC; ++j) o[j] = f32x4_k{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < NR; ++k) {
+    m[k] = -INFINITY;
+    lsum[k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) o[k][j] = f32x4_k{0.f, 0.f, 0.f, 0.f};
+  }
 
   if (v0 < v1) {
     // queries as the B operand, channels in the order the key loads have them
-    bf16x8_k qf[KS][QP];
+    bf16x8_k qf[NR][KS][QP];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int ch = FMT == KV_BF16 ? 32 * ks + 8 * g : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
-      float x[8];
-      load8(static_cast<const typename std::conditional<sizeof(IO) == 4, float, uint16_t>::type *>(a.q) + q_at + ch, x);
-      split_parts<QP>(x, qf[ks]);
-    }
+    for (int k = 0; k < NR; ++k)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int ch = FMT == KV_BF16 ? 32 * ks + 8 * g : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
+        float x[8];
+        load8(static_cast<const IO *>(a.q) + q_at[k] + ch, x);
+        split_parts<QP>(x, qf[k][ks]);
+      }
     const uint32_t row_bytes = uint32_t(a.Hkv) * D * ES;
     const int64_t layer = int64_t(l) * a.num_slots;
     // wave-uniform bases; a row is a per-lane byte offset, 32 bits wide where a layer is below 4 GB
@@ -155,7 +168,9 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
     };
     bool odd = false;                              // a value that is not finite was left out
     auto compute = [&](Block &x, int base) __attribute__((always_inline)) {
-      f32x4_k acc[2] = {f32x4_k{0.f, 0.f, 0.f, 0.f}, f32x4_k{0.f, 0.f, 0.f, 0.f}};
+      f32x4_k acc[NR][2];
+#pragma unroll
+      for (int k = 0; k < NR; ++k) acc[k][0] = acc[k][1] = f32x4_k{0.f, 0.f, 0.f, 0.f};
       if constexpr (FMT != KV_BF16) {
         if (lane < FEW_BLOCK) {
           sc[w][0][lane] = x.s.x * to_log2;
@@ -175,7 +190,10 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
           }
           const bf16x8_k kf = __builtin_bit_cast(bf16x8_k, u);
 #pragma unroll
-          for (int p = QP - 1; p >= 0; --p) acc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks][p], acc[kb], 0, 0, 0);
+          for (int k = 0; k < NR; ++k)
+#pragma unroll
+            for (int p = QP - 1; p >= 0; --p)
+              acc[k][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[k][ks][p], acc[k][kb], 0, 0, 0);
         }
       float4 vs[2];
       if constexpr (FMT != KV_BF16) {
@@ -185,64 +203,65 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         for (int kb = 0; kb < 2; ++kb) {
           const float4 ks = *reinterpret_cast<const float4 *>(&sc[w][0][16 * kb + 4 * g]);
           vs[kb] = *reinterpret_cast<const float4 *>(&sc[w][1][16 * kb + 4 * g]);
-          acc[kb][0] *= ks.x;
-          acc[kb][1] *= ks.y;
-          acc[kb][2] *= ks.z;
-          acc[kb][3] *= ks.w;
+#pragma unroll
+          for (int k = 0; k < NR; ++k) acc[k][kb] *= f32x4_k{ks.x, ks.y, ks.z, ks.w};
         }
         __builtin_amdgcn_wave_barrier();
       } else {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) acc[kb] *= to_log2;
+        for (int k = 0; k < NR; ++k) acc[k][0] *= to_log2, acc[k][1] *= to_log2;
       }
       // a block that every token sees whole needs no mask: its last entry is at or before the
       // oldest token's own, and its first inside the newest's window or all of it among the sinks
       const int last = base + FEW_BLOCK - 1, oldest = N - n;
       const int jl = last < first ? last : last + gap, j0 = base < first ? base : base + gap;
       const bool whole = last < v1 && jl <= oldest && (a.window == 0 || jl < a.sinks || j0 > N - 1 - a.window);
-      uint32_t hidden = 0;                         // bit 4 kb + i: not seen by this lane's row
-      if (!whole) {
+      bf16x8_k pf[NR][PP];
+#pragma unroll
+      for (int k = 0; k < NR; ++k) {
+        uint32_t hidden = 0;                       // bit 4 kb + i: not seen by this row
+        if (!whole) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int v = base + 16 * kb + 4 * g + i, j = v < first ? v : v + gap;
+              const bool see = (v < v1) & (j <= own[k]) & ((a.window == 0) | (j < a.sinks) | (j > own[k] - a.window));
+              hidden |= see ? 0u : 1u << (4 * kb + i);
+              acc[k][kb][i] = see ? acc[k][kb][i] : -INFINITY;
+            }
+        }
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, acc[k][kb][i]);
+        if (__builtin_amdgcn_ballot_w64(!(tmax - m[k] <= FEW_SLACK)) != 0) {
+          tmax = fmaxf(tmax, __shfl_xor(tmax, 16, WAVE));
+          tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
+          const float mn = fmaxf(m[k], tmax);
+          const float corr = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - mn);
+          m[k] = mn;
+          lsum[k] *= corr;
+#pragma unroll
+          for (int j = 0; j < NC; ++j) o[k][j] *= corr;
+        }
+        float pw[8];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int v = base + 16 * kb + 4 * g + i, j = v < first ? v : v + gap;
-            const bool see = (v < v1) & (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
-            hidden |= see ? 0u : 1u << (4 * kb + i);
-            acc[kb][i] = see ? acc[kb][i] : -INFINITY;
+            float p = __builtin_amdgcn_exp2f(acc[k][kb][i] - m[k]);
+            if (hidden >> (4 * kb + i) & 1) p = 0.f;
+            lsum[k] += p;
+            if constexpr (FMT != KV_BF16) {
+              p *= (&vs[kb].x)[i];
+              if (hidden >> (4 * kb + i) & 1) p = 0.f;      // the scale of an unseen row may be anything
+            }
+            pw[4 * kb + i] = p;
           }
+        split_parts<PP>(pw, pf[k]);
       }
-      float tmax = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, acc[kb][i]);
-      if (__builtin_amdgcn_ballot_w64(!(tmax - m <= FEW_SLACK)) != 0) {
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 16, WAVE));
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
-        const float mn = fmaxf(m, tmax);
-        const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        lsum *= corr;
-#pragma unroll
-        for (int j = 0; j < NC; ++j) o[j] *= corr;
-      }
-      float pw[8];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float p = __builtin_amdgcn_exp2f(acc[kb][i] - m);
-          if (hidden >> (4 * kb + i) & 1) p = 0.f;
-          lsum += p;
-          if constexpr (FMT != KV_BF16) {
-            p *= (&vs[kb].x)[i];
-            if (hidden >> (4 * kb + i) & 1) p = 0.f;        // the scale of an unseen row may be anything
-          }
-          pw[4 * kb + i] = p;
-        }
-      bf16x8_k pf[PP];
-      split_parts<PP>(pw, pf);
       if constexpr (FMT == KV_BF16) {
         if (!whole) {
 #pragma unroll
@@ -275,8 +294,10 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         for (int i = 0; i < STEP; ++i) {
           const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(f[i][0], f[i][1], f[i][2], f[i][3]));
 #pragma unroll
-          for (int p = PP - 1; p >= 0; --p)
-            o[STEP * k + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[p], o[STEP * k + i], 0, 0, 0);
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int p = PP - 1; p >= 0; --p)
+              o[r][STEP * k + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][p], o[r][STEP * k + i], 0, 0, 0);
         }
       }
     };
@@ -306,81 +327,102 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       if (__builtin_amdgcn_ballot_w64(odd) != 0)
         for (int v = v0; v < v1; ++v) {
           const int e = v < first ? v : v + gap;
-          const bool see = (e <= own) & ((a.window == 0) | (e < a.sinks) | (e > own - a.window));
           const uint16_t *row = reinterpret_cast<const uint16_t *>(vbase + row_at(list[e], 0));
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int k = 0; k < NR; ++k) {
+            const bool see = (e <= own[k]) & ((a.window == 0) | (e < a.sinks) | (e > own[k] - a.window));
 #pragma unroll
-            for (int j = 0; j < NC; ++j) {
-              const uint16_t y = row[NC * (4 * g + i) + j];
-              o[j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
-            }
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < NC; ++j) {
+                const uint16_t y = row[NC * (4 * g + i) + j];
+                o[k][j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+              }
+          }
         }
     }
   }
-  lsum += __shfl_xor(lsum, 16, WAVE);
-  lsum += __shfl_xor(lsum, 32, WAVE);
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    lsum[k] += __shfl_xor(lsum[k], 16, WAVE);
+    lsum[k] += __shfl_xor(lsum[k], 32, WAVE);
+  }
   if (parts_wg > 1) {
     // the other waves of a head leave their state in LDS, lane for lane; the first joins them
-    float *mine = joint + (w - heads) * (4 * NC + 2) * WAVE + lane;
+    constexpr int STATE = (4 * NC + 2) * WAVE;
     if (part_wg > 0) {
-      mine[0] = m;
-      mine[WAVE] = lsum;
 #pragma unroll
-      for (int j = 0; j < NC; ++j)
+      for (int k = 0; k < NR; ++k) {
+        float *mine = joint + ((w - heads) * NR + k) * STATE + lane;
+        mine[0] = m[k];
+        mine[WAVE] = lsum[k];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mine[(2 + 4 * j + i) * WAVE] = o[j][i];
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine[(2 + 4 * j + i) * WAVE] = o[k][j][i];
+      }
     }
     __syncthreads();
     if (part_wg > 0) return;
     for (int p = 1; p < parts_wg; ++p) {
-      const float *x = joint + (w + (p - 1) * heads) * (4 * NC + 2) * WAVE + lane;
-      const float mp = x[0], mn = fmaxf(m, mp);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      const float fp = mp == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mp - mn);
-      m = mn;
-      lsum = lsum * f + x[WAVE] * fp;
 #pragma unroll
-      for (int j = 0; j < NC; ++j)
+      for (int k = 0; k < NR; ++k) {
+        const float *x = joint + ((w + (p - 1) * heads) * NR + k) * STATE + lane;
+        const float mp = x[0], mn = fmaxf(m[k], mp);
+        const float f = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - mn);
+        const float fp = mp == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mp - mn);
+        m[k] = mn;
+        lsum[k] = lsum[k] * f + x[WAVE] * fp;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] = o[j][i] * f + x[(2 + 4 * j + i) * WAVE] * fp;
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[k][j][i] = o[k][j][i] * f + x[(2 + 4 * j + i) * WAVE] * fp;
+      }
     }
   }
-  if (c >= rows) return;
-  if (nsplit == 1) {
-    const float inv = m == -INFINITY ? 0.f : 1.0f / lsum;      // nothing seen: zero
-    IO *out = static_cast<IO *>(a.out) + q_at;
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    const int r = 16 * k + c;
+    if (r >= rows) continue;
+    if (nsplit == 1) {
+      const float inv = m[k] == -INFINITY ? 0.f : 1.0f / lsum[k];      // nothing seen: zero
+      IO *out = static_cast<IO *>(a.out) + q_at[k];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NC; ++j) out[NC * (4 * g + i) + j] = Store<IO>::from(o[k][j][i] * inv);
+      continue;
+    }
+    const int64_t part = (((int64_t(b) * a.L + l) * a.Hkv + hkv) * nsplit + split) * rows_max + r;
+    const int64_t parts = int64_t(gridDim.z) * a.L * a.Hkv * nsplit * rows_max;
+    float *po = a.ws + part * D;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < NC; ++j) out[NC * (4 * g + i) + j] = Store<IO>::from(o[j][i] * inv);
-    return;
+      for (int j = 0; j < NC; j += 4)
+        *reinterpret_cast<float4 *>(po + NC * (4 * g + i) + j) =
+            make_float4(o[k][j][i], o[k][j + 1][i], o[k][j + 2][i], o[k][j + 3][i]);
+    if (g == 0) *reinterpret_cast<float2 *>(a.ws + parts * D + part * 2) = make_float2(m[k], lsum[k]);
   }
-  const int64_t part = (((int64_t(b) * a.L + l) * a.Hkv + hkv) * nsplit + split) * rows_max + c;
-  const int64_t parts = int64_t(gridDim.z) * a.L * a.Hkv * nsplit * rows_max;
-  float *po = a.ws + part * D;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < NC; j += 4)
-      *reinterpret_cast<float4 *>(po + NC * (4 * g + i) + j) = make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
-  if (g == 0) *reinterpret_cast<float2 *>(a.ws + parts * D + part * 2) = make_float2(m, lsum);
 }
 
-template <int FMT, typename IO, int D>
+template <int FMT, typename IO, int D, int NR>
 static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   KTimer kt_("k_attend_few", st);
   const dim3 grid(unsigned(p.splits), unsigned(a.L * (a.Hkv / p.heads)), unsigned(a.B));
-  const size_t lds = size_t(p.parts - 1) * p.heads * (D / 4 + 2) * WAVE * sizeof(float);
+  const size_t lds = size_t(p.parts - 1) * p.heads * NR * (D / 4 + 2) * WAVE * sizeof(float);
   if (a.num_slots * a.Hkv * D * (FMT == KV_BF16 ? 2 : 1) < (int64_t(1) << 32))
-    k_attend_few<FMT, IO, D, true><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
+    k_attend_few<FMT, IO, D, NR, true><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
   else
-    k_attend_few<FMT, IO, D, false><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
+    k_attend_few<FMT, IO, D, NR, false><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
 }
 
 template <int FMT, typename IO>
 static void go_few_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  a.D == 128 ? go_few<FMT, IO, 128>(a, p, st) : go_few<FMT, IO, 64>(a, p, st);
+  if constexpr (FMT != KV_BF16 && sizeof(IO) == 2) {
+    if (p.rows > 16) return a.D == 128 ? go_few<FMT, IO, 128, 2>(a, p, st) : go_few<FMT, IO, 64, 2>(a, p, st);
+  }
+  a.D == 128 ? go_few<FMT, IO, 128, 1>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
 }
 
 hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
