@@ -441,7 +441,8 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *             one: the code does not depend on the precision it is computed in);
  *   IKV_E4M3  scale = the least power of two with 448 scale >= a, code_d = x_d / scale
  *             rounded to the nearest E4M3 value, ties to even. A power of two costs a
- *             floating code no precision, and makes reading back exact, in bf16 too.
+ *             floating code no precision, and makes reading back exact, in bf16 too; the
+ *             calls take the scales of E4M3 rows as powers of two, whoever wrote them.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
  * every channel. L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
  * of a larger cache is a descriptor with L = 1 and pointers to that layer.
@@ -469,7 +470,8 @@ typedef struct ikv_quant_pool {
  *        are not listed stay as they are.
  *   n_rows: device int32 [B], or NULL: N rows per session; values are clamped to [0, N].
  * pool and cache must agree in L, Hkv and D (IKV_ESHAPE); the pool's rows are bf16 or
- * float32, 16-byte aligned. Needs no workspace. Only N and slot_off of the sessions are read.
+ * float32, 16-byte aligned. At most 2^24 - 1 rows per session, 65535 sessions and layers
+ * (IKV_EUNSUPPORTED). Needs no workspace. Only N and slot_off of the sessions are read.
  */
 ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool,
                            const ikv_session *sess, const ikv_session *sess_dev, int32_t B,
@@ -509,6 +511,8 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
  *     (IKV_EUNSUPPORTED otherwise). q and out may not overlap.
  *   workspace: ikv_workspace_bytes / ikv_quant_workspace_bytes with IKV_CALL_DECODE or
  *     IKV_CALL_CHUNK (the same for every sinks and window).
+ *   At most 2^30 entries per list, 65535 sessions, 65535 = L * Hq, and chunks whose row blocks
+ *   (256 rows of a KV head) of the whole batch stay under 2^23 (IKV_EUNSUPPORTED).
  *   As with ikv_decode_attend_slotmap, long lists are split across workgroups by bounds known
  *   on the host, min(N, max(C, pi + qe - qs)) entries for the decode and N for the chunk calls;
  *   the order of the sums depends on them.

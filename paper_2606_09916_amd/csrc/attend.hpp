@@ -26,7 +26,7 @@ struct AttendArgs {
   bool decode;             // one token per session, whatever its span
   const void *q;
   const int32_t *live, *n_live;
-  int sinks, window;       // window 0: none (and sinks 0)
+  int sinks, window;       // at most ATTEND_MOST; window 0: none (and sinks 0)
   void *out;
   float *ws;
 };
@@ -35,6 +35,7 @@ constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wa
                                     // over the 8-bit cache with bf16 outputs)
 constexpr int FEW_WAVES = 8;        // of a workgroup of k_attend_few, at most
 constexpr int CUS = 256;            // a round: one workgroup on each
+constexpr int ATTEND_MOST = 1 << 30;       // entries of a list, rows of a KV head, sinks and window
 constexpr int TILE_KEYS = 64;       // entries per tile of k_attend_tile
 
 struct AttendPlan {
@@ -126,7 +127,7 @@ inline int attend_tile_splits(int64_t wgs, int rows, int blocks, int64_t longest
 inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int B, bool decode, int sinks, int window) {
   AttendPlan p{};
   const int G = a.Hq / a.Hkv;
-  int64_t longest = 1, sum = 0;
+  int64_t longest = 1, sum = 0, most = 0;
   for (int b = 0; b < B; ++b) {
     const int n = attend_tokens(sess[b], decode);
     p.max_n = std::max(p.max_n, n);
@@ -134,6 +135,7 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     if (window) len = std::min<int64_t>(len, int64_t(sinks) + window + n);
     longest = std::max(longest, len);
     sum += len;
+    most = std::max<int64_t>(most, sess[b].N);
   }
   p.few = int64_t(p.max_n) * G <= (a.format != KV_BF16 && !a.io_f32 ? 2 * FEW_ROWS : FEW_ROWS);
   p.splits = p.blocks = 1;
@@ -150,7 +152,10 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
   // the workspace is sized without the window
   if (window) p.splits = std::min(p.splits, attend_plan(a, sess, B, decode, 0, 0).splits);
   if (p.splits > 1) p.ws_floats = int64_t(B) * a.L * a.Hkv * p.blocks * p.splits * p.rows * (a.D + 2);
-  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || int64_t(B) * a.L * a.Hkv * p.blocks > (1 << 24);
+  // launch grids: 65535 in y and z, under 2^32 threads in x; entries and rows stay below 2^30
+  const int64_t threads = (groups * a.Hkv + 7) / 8 * 8 * p.blocks * p.splits * 2 * p.rows;
+  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || most > ATTEND_MOST || int64_t(p.max_n) * G > ATTEND_MOST ||
+                (!p.few && threads >= int64_t(1) << 32);
   return p;
 }
 

@@ -308,11 +308,11 @@ ikv_status attend(ikv::AttendArgs a, const ikv_session *sess, const ikv_session 
   if ((r = check_ws(workspace, workspace_bytes, attend_bytes(a, sess, B, decode)))) return r;
   const ikv::AttendPlan plan = ikv::attend_plan(a, sess, B, decode, sinks, window);
   if (plan.max_n == 0) return ok();
-  if (plan.too_large) return fail(IKV_EUNSUPPORTED, "%s: too many sessions, layers and query rows for one launch", what);
+  if (plan.too_large) return fail(IKV_EUNSUPPORTED, "%s: too many sessions, layers, entries or query rows for one launch", what);
   if (debug_mode() && (r = debug_live(sess, B, live, n_live, a.num_slots, (hipStream_t)stream))) return r;
   a.sess = sess_dev, a.B = B, a.decode = decode;
   a.q = q, a.live = live, a.n_live = n_live, a.out = out;
-  a.sinks = window ? sinks : 0, a.window = window;
+  a.sinks = window ? std::min(sinks, ikv::ATTEND_MOST) : 0, a.window = std::min(window, ikv::ATTEND_MOST);
   a.ws = static_cast<float *>(workspace);
   return hip_status(ikv::launch_attend(a, plan, (hipStream_t)stream), what);
 }
@@ -330,7 +330,8 @@ ikv_status check_quant_rows(const ikv_quant_pool *c, const ikv_pool *p, const ik
   if ((reinterpret_cast<uintptr_t>(p->k_pool) | reinterpret_cast<uintptr_t>(p->v_pool)) % 16)
     return fail(IKV_EINVAL, "pool: k_pool and v_pool must be 16-byte aligned");
   if ((r = check_sessions(sess, sess_dev, B))) return r;
-  if (B > 65535) return fail(IKV_EUNSUPPORTED, "B = %d > 65535", B);
+  if (B > 65535 || c->L > 65535 || max_n(sess, B) > ikv::QUANT_MOST)
+    return fail(IKV_EUNSUPPORTED, "more than 65535 sessions or layers, or %d rows of a session", ikv::QUANT_MOST);
   if (B > 0 && !cache_ids) return fail(IKV_EINVAL, "%s is NULL", cache_what);
   if (!pool_ids)
     for (int b = 0; b < B; ++b)

@@ -30,19 +30,18 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_attend_merge(AttendArgs a, in
   for (int z = 0; z < nsplit; ++z) M = fmaxf(M, ml[int64_t(z) * rows].x);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
-  if (M != -INFINITY)
 #pragma unroll 4
-    for (int z = 0; z < nsplit; ++z) {
-      const float4 x = *reinterpret_cast<const float4 *>(a.ws + (part + int64_t(z) * rows) * D + d);
-      const float2 y = ml[int64_t(z) * rows];
-      const float f = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - M);
-      acc.x = fmaf(x.x, f, acc.x);
-      acc.y = fmaf(x.y, f, acc.y);
-      acc.z = fmaf(x.z, f, acc.z);
-      acc.w = fmaf(x.w, f, acc.w);
-      sum = fmaf(y.y, f, sum);
-    }
-  const float inv = M == -INFINITY ? 0.f : 1.0f / sum;
+  for (int z = 0; z < nsplit; ++z) {
+    const float4 x = *reinterpret_cast<const float4 *>(a.ws + (part + int64_t(z) * rows) * D + d);
+    const float2 y = ml[int64_t(z) * rows];
+    const float f = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - M);
+    acc.x = fmaf(x.x, f, acc.x);
+    acc.y = fmaf(x.y, f, acc.y);
+    acc.z = fmaf(x.z, f, acc.z);
+    acc.w = fmaf(x.w, f, acc.w);
+    sum = fmaf(y.y, f, sum);
+  }
+  const float inv = M == -INFINITY ? 1.0f : 1.0f / sum;      // nothing seen: the states are zero (NaN where a query is)
   const int t = R / G, h = R - t * G;
   IO *o = static_cast<IO *>(a.out) + before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D + d;
   if constexpr (sizeof(IO) == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);

@@ -239,7 +239,7 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         if (__builtin_amdgcn_ballot_w64(!(tmax - m[k] <= FEW_SLACK)) != 0) {
           tmax = fmaxf(tmax, __shfl_xor(tmax, 16, WAVE));
           tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
-          const float mn = fmaxf(m[k], tmax);
+          const float mn = !(tmax - m[k] <= FEW_SLACK) ? fmaxf(m[k], tmax) : m[k];     // by this row alone
           const float corr = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - mn);
           m[k] = mn;
           lsum[k] *= corr;

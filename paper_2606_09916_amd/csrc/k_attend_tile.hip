@@ -288,7 +288,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       if constexpr (FMT != KV_INT8) tmax *= to_log2;
       if (__builtin_amdgcn_ballot_w64(!(tmax - m <= TILE_SLACK)) != 0) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32, WAVE));
-        const float mn = fmaxf(m, tmax);
+        const float mn = !(tmax - m <= TILE_SLACK) ? fmaxf(m, tmax) : m;     // by this row alone
         const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         lsum *= corr;

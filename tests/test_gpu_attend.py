@@ -298,3 +298,67 @@ def test_debug_mode_names_bad_entries(dev, monkeypatch):
         s.run(q)
     with pytest.raises(ikv.IkvError, match=r"session 1: live\[5\]"):
         s.run(s.queries(2), decode=True)
+
+
+@pytest.mark.parametrize("code", ["int8", "bf16"])
+@pytest.mark.parametrize("n,n_live", [(3, [0, 2, 200]), (60, [1, 59, 200])])
+def test_the_largest_window_and_sinks(dev, code, n, n_live):
+    s = Setup(dev, code, "bf16", 1, 4, 1, 128, [200] * 3, n, n_live=n_live)
+    q = s.queries(3 * n)
+    big = 2 ** 31 - 1
+    for sinks, window in ((0, big), (big, big), (big, 1), (0, 200)):
+        s.check(s.run(q, sinks, window), q, [n] * 3, sinks, window)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3", "bf16"])
+@pytest.mark.parametrize("N,n", [(40, 2), (5000, 1), (5000, 6), (300, 90), (6000, 40)])
+def test_a_query_that_is_not_finite_spoils_its_row_only(dev, code, N, n):
+    import torch
+    s = Setup(dev, code, "bf16", 1, 4, 1, 128, [N], n)
+    q = s.queries(n)
+    clean = s.run(q).view(4, n, 128)
+    q.view(4, n, 128)[2, n // 2, 7] = float("nan")
+    out = s.run(q).view(4, n, 128)
+    bad = torch.zeros(4, n, dtype=torch.bool, device=dev)
+    bad[2, n // 2] = True
+    assert out[bad].isnan().all() and torch.equal(out[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("code,Hkv,D,slots", [("int8", 8, 128, 4_300_000), ("bf16", 8, 128, 2_200_000),
+                                              ("e4m3", 1, 64, 17_000_000)])
+def test_offsets_past_32_bits_and_many_slots(dev, code, Hkv, D, slots):
+    """A layer of more than 4 GB, and more than 2^24 slots: rows at the far end."""
+    import torch
+    N, G = 700, 2
+    s = Setup(dev, code, "bf16", 1, G * Hkv, Hkv, D, [N], 40)
+    far = s.live.clone()
+    far[::2] = slots - 1 - far[::2]
+    big = [torch.empty(1, slots, Hkv, D, dtype=s.k.dtype, device=dev) for _ in range(2)]
+    for x, y in zip(big, (s.k, s.v)):
+        raw = torch.int16 if code == "bf16" else torch.int8
+        x.view(raw)[0, far.long()] = y.view(raw)[0, s.live.long()]
+    a = (1, G * Hkv, Hkv, D, slots, 0)
+    if code != "bf16":
+        sc = torch.empty(1, slots, Hkv, 2, device=dev)
+        sc[0, far.long()] = s.sc[0, s.live.long()]
+    t = Setup(dev, code, "bf16", 1, G * Hkv, Hkv, D, [N], 40)
+    t.live = far
+    t.pool = ikv.make_pool(*big, *a) if code == "bf16" else ikv.make_quant_pool(*big, sc, *a)
+    t5, s5 = (sessions([N], dev, 5) for _ in range(2))
+    for n, st, ss in ((40, t.sess, s.sess), (5, t5, s5)):
+        t.sess, s.sess = st, ss
+        q = s.queries(n)
+        assert torch.equal(t.run(q, 3, 300), s.run(q, 3, 300))
+    if code == "bf16":
+        return
+    q = s.queries(1)
+    assert torch.equal(t.run(q, decode=True), s.run(q, decode=True))
+    # written and read back there
+    k = torch.randn(1, N, Hkv, D, device=dev).bfloat16()
+    rows = ikv.make_pool(k, k, 1, Hkv, Hkv, D, N, 0)
+    ikv.quant_store(t.pool, rows, t.sess, None, far)
+    back = torch.zeros_like(k)
+    ikv.quant_load(t.pool, ikv.make_pool(back, back.clone(), 1, Hkv, Hkv, D, N, 0), t.sess, far)
+    c, w = qo.quantise(k[0].double().cpu().numpy(), code)
+    want = torch.from_numpy(qo.code_values(c, code).astype(np.float32) * w[..., None]).bfloat16()
+    assert torch.equal(back[0].cpu(), want)

@@ -85,6 +85,16 @@ def test_row_calls(call):
     assert call(s=_sess(N=0, qs=0, qe=0)) == 0          # no rows: nothing is launched
 
 
+def test_sizes_past_a_launch():
+    big = _sess(N=1 << 24, qs=0, qe=1)
+    assert _store(p=_pool(num_slots=1 << 25), s=big) == EUNSUPPORTED
+    assert _load(p=_pool(num_slots=1 << 25), s=big) == EUNSUPPORTED
+    assert _store(_cache(L=70000), _pool(L=70000)) == EUNSUPPORTED
+    assert _attend("decode", _cache(L=20000)) == EUNSUPPORTED
+    assert _attend("decode", s=_sess(N=(1 << 30) + 1, qs=0, qe=1)) == EUNSUPPORTED
+    assert _attend("chunk", s=_sess(N=1 << 29, qs=0, qe=1 << 29)) == EUNSUPPORTED
+
+
 def test_rows_of_an_identity_list_must_fit():
     assert _store(dst=None) == EINVAL and _load(src=None) == EINVAL
     assert _store(s=_sess(slot_off=60), src=None) == ESHAPE
