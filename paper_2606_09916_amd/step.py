@@ -98,6 +98,23 @@ class RetentionStep:
     def decode(self):
         ikv.decode_attend_slotmap(self.pool, self.sess, self.q_dec, self.live, self.n_live, self.out, self.ws)
 
+    def quantise(self, code: str = "int8"):
+        """Put the rows of the live slots into an 8-bit cache of the pool's shape ("int8" or "e4m3"), same slots:
+        the decode over it reads half the bytes, and the pool can go."""
+        import torch
+        ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
+        if getattr(self, "k_codes", None) is None or self.k_codes.dtype != ct:
+            shape = (self.L, self.num_slots, self.Hkv, self.D)
+            self.k_codes, self.v_codes = (torch.empty(shape, dtype=ct, device=self.device) for _ in range(2))
+            self.code_scales = torch.empty((*shape[:3], 2), dtype=torch.float32, device=self.device)
+            self.cache = ikv.make_quant_pool(self.k_codes, self.v_codes, self.code_scales, self.L, self.Hq, self.Hkv,
+                                             self.D, self.num_slots, self.dead, io_dtype=self.q_dec.dtype)
+        ikv.quant_store(self.cache, self.pool, self.sess, self.live, self.live, self.n_live)
+
+    def decode_quant(self, sinks: int = 0, window: int = 0):
+        ikv.decode_attend_quant(self.cache, self.sess, self.q_dec, self.live, self.n_live, self.out, self.ws,
+                                sinks=sinks, window=window)
+
     def step(self, update_memory: bool = True):
         if update_memory:
             self.qm_update()

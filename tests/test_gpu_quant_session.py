@@ -92,3 +92,38 @@ def test_session(dev, code):
     want = oracle.scores(k_host, S, sets, st.M.cpu().numpy().reshape(L, Hkv * 16, D), Hkv, 16)
     c = sets["cand"]
     assert np.all(np.abs(scores.cpu().numpy()[c] - want[c]) <= 1e-3 * np.abs(want[c]) + 1e-6 * np.abs(want[c]).max())
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("D,kv", [(128, synth.BF16), (64, synth.F32)])
+def test_step_quantises_what_it_keeps(dev, code, D, kv):
+    """RetentionStep.quantise and decode_quant after an event, two sessions, both pool types."""
+    L, Hq, Hkv = 2, 8, 2
+    specs = [synth.SessionSpec(N=900, C=200, pi=4, qs=868, qe=900, R=16, dead_frac=0.1),
+             synth.SessionSpec(N=500, C=300, pi=0, qs=468, qe=500, R=16, dead_frac=0.0)]
+    batch = synth.make_batch(synth.Shape(L=L, Hq=Hq, Hkv=Hkv, D=D), specs, seed=82, kv_dtype=kv, layout="paged")
+    st = RetentionStep(batch, dev)
+    st.init_dead_slot()
+    st.step()
+    full = st.host("out")
+    st.quantise(code)
+    u, P = (2.0 ** -8, 2.0 ** -8) if kv == synth.BF16 else (2.0 ** -24, 2.0 ** -22)
+    for sinks, window in ((0, 0), (3, 64)):
+        st.decode_quant(sinks, window)
+        for b in range(2):
+            off, n = st.sess[b].slot_off, int(st.n_live[b])
+            at = st.live[off:off + n].long()
+            for l in range(L):
+                k, v = (qo.code_values(c[l].view(torch_uint8())[at].cpu().numpy(), code)
+                        * st.code_scales[l][at][..., i].double().cpu().numpy()[..., None]
+                        for i, c in enumerate((st.k_codes, st.v_codes)))
+                want, A, X = qo.attend(st.q_dec[b, l].double().cpu().numpy()[:, None], k, v, sinks, window)
+                E = ((D + 8) * X + 4 * (1 + X) + n + 8) * 2.0 ** -24
+                tol = u * np.abs(want) + (P + 2 * E[..., None]) * A
+                assert np.all(np.abs(st.out[b, l].double().cpu().numpy()[:, None] - want) <= tol)
+    assert full.shape == st.host("out").shape
+
+
+def torch_uint8():
+    import torch
+    return torch.uint8
