@@ -3,7 +3,8 @@
 // the 8-bit cache with bf16 outputs (the other types' registers hold one).
 //
 // Bound by reading the rows of the list once (2 D + 8 bytes per entry, head and layer in
-// 8-bit form, 4 D in bf16). A wave owns one KV head and a split of the list and keeps
+// 8-bit form, 4 D in bf16): 36 layers x 8 heads x 8192 int8 entries in 105 us (5.9 TB/s), bf16
+// 187 us (6.4), 48 x 8 x 92,300 int8 in 1.49 ms (6.3). A wave owns one KV head and a split of the list and keeps
 // everything in registers; the waves of a workgroup own adjacent heads, so together they
 // read whole pieces of 4 rows. It walks blocks of 32 entries, the next block's rows on
 // their way while one is computed:
@@ -139,6 +140,8 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       const int v = min(base + (lane & 31), v1 - 1);
       return list[v < first ? v : v + gap];
     };
+    // Value rows go past the caches (nothing reads them again: 123 -> 113 us at 8192 entries); key
+    // rows do not, since two loads of 64 bytes share each of their lines (so: 121).
     auto load = [&](Block &x, int sl) __attribute__((always_inline)) {
       if constexpr (FMT != KV_BF16)                // in the order of use
         x.s = *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(sbase) + row_at(sl, 0) / (D / 8));

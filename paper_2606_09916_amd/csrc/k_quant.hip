@@ -96,7 +96,9 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
 // A workgroup takes `group` list entries of one layer; an entry is `per` = Hkv D / 8 threads'
 // work, a thread's 8 channels of its K and of its V row. A thread takes QU places at a time,
 // all their slots loaded first, then all their rows: bound by memory, the kernels need that
-// many bytes in flight per CU.
+// many bytes in flight per CU. 8192 rows of 36 layers x 8 heads, D = 128, bf16, E4M3: stored in
+// 350 us (5.2 TB/s read and written), read back in 311 (5.9); with one place a thread both took
+// 1331, with eight 666.
 constexpr int QU = 4;
 
 template <typename T, int D>
