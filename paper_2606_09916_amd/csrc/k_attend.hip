@@ -41,8 +41,9 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_attend_merge(AttendArgs a, in
     acc.w = fmaf(x.w, f, acc.w);
     sum = fmaf(y.y, f, sum);
   }
-  const float inv = M == -INFINITY ? 1.0f : 1.0f / sum;      // nothing seen: the states are zero (NaN where a query is)
   const int t = R / G, h = R - t * G;
+  const bool sees = max(0, min(a.n_live[b], s.N)) - n + t >= 0;
+  const float inv = sees ? 1.0f / sum : 0.f;                 // nothing seen: zero
   IO *o = static_cast<IO *>(a.out) + before * a.L * a.Hq * D + ((int64_t(l) * a.Hq + hkv * G + h) * n + t) * D + d;
   if constexpr (sizeof(IO) == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   else {

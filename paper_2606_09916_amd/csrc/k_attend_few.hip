@@ -249,13 +249,13 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
 #pragma unroll
           for (int j = 0; j < NC; ++j) o[k][j] *= corr;
         }
+        const float ms = m[k] == -INFINITY ? 0.f : m[k];     // no logit above -inf yet: the weights are 2^-inf
         float pw[8];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float p = __builtin_amdgcn_exp2f(acc[k][kb][i] - m[k]);
-            if (hidden >> (4 * kb + i) & 1) p = 0.f;
+            float p = __builtin_amdgcn_exp2f(acc[k][kb][i] - ms);
             lsum[k] += p;
             if constexpr (FMT != KV_BF16) {
               p *= (&vs[kb].x)[i];
@@ -388,7 +388,7 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
     const int r = 16 * k + c;
     if (r >= rows) continue;
     if (nsplit == 1) {
-      const float inv = m[k] == -INFINITY ? 0.f : 1.0f / lsum[k];      // nothing seen: zero
+      const float inv = own[k] < 0 ? 0.f : 1.0f / lsum[k];             // nothing seen: zero
       IO *out = static_cast<IO *>(a.out) + q_at[k];
 #pragma unroll
       for (int i = 0; i < 4; ++i)

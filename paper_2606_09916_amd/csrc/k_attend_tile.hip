@@ -8,7 +8,8 @@
 // E4M3 2.38; 14B, 1024 tokens, bf16, window 4096, 4.13 TFLOP: 4.06 ms. 256 rows: of 128, four
 // waves, two workgroups a CU stage every tile twice as often (3.06 ms against 2.82); of 64 rows a
 // wave the registers spill (6.0 ms).
-//   staging   rows or codes go from HBM through registers, are made bf16 (codes exactly) and
+//   staging   rows or codes go from HBM through registers, are made bf16 (exactly:
+//             int8 codes as they are, E4M3 ones with their scales, which are powers of two) and
 //             written to one of two LDS buffers, the keys a tile before the values: keys
 //             [64][D + 8], values [64][D + 32], strides that spread the reads over all banks
 //   S^T = K Q^T with 32 x 32 x 16 products: lane (h, c) holds entries 8 i + 4 h + (0..3) of
@@ -79,13 +80,11 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   const int rb = blocks - 1 - in / nsplit, split = in % nsplit;
   const int hkv = unit % a.Hkv, l = unit / a.Hkv % a.L, b = unit / a.Hkv / a.L;
   const ikv_session s = a.sess[b];
-  const int G = a.Hq / a.Hkv, n = a.decode ? 1 : s.qe - s.qs, rows = n * G;
+  const int G = a.Hq / a.Hkv, n = s.qe - s.qs, rows = n * G;
   const int row0 = rb * ROWS;
   if (row0 >= rows) return;
   int64_t before = 0;
-  if (a.decode) before = b;
-  else
-    for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
+  for (int i = 0; i < b; ++i) before += a.sess[i].qe - a.sess[i].qs;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h2 = lane >> 5, c = lane & 31;
   const int row = row0 + 32 * w + c, rr = min(row, rows - 1);
@@ -299,7 +298,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] *= corr;
       }
-      const float ms = m == -INFINITY ? 0.f : m;   // a row that has seen nothing: its weights are 2^-inf
+      const float ms = m == -INFINITY ? 0.f : m;   // no logit above -inf yet: the weights are 2^-inf
       store(r, tile + 1, par ^ 1);
       load(ko, vo, r);
 #pragma unroll
@@ -434,7 +433,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   lsum += __shfl_xor(lsum, 32, WAVE);
   if (row >= rows) return;
   if (nsplit == 1) {
-    const float inv = m == -INFINITY ? 0.f : 1.0f / lsum;      // nothing seen: zero
+    const float inv = own < 0 ? 0.f : 1.0f / lsum;             // nothing seen: zero
     IO *out = static_cast<IO *>(a.out) + q_at;
 #pragma unroll
     for (int db = 0; db < DB; ++db)

@@ -362,3 +362,30 @@ def test_offsets_past_32_bits_and_many_slots(dev, code, Hkv, D, slots):
     c, w = qo.quantise(k[0].double().cpu().numpy(), code)
     want = torch.from_numpy(qo.code_values(c, code).astype(np.float32) * w[..., None]).bfloat16()
     assert torch.equal(back[0].cpu(), want)
+
+
+@pytest.mark.parametrize("N,m,n", [(400, 97, 2), (400, 160, 20), (500, 130, 70), (3000, 1600, 3), (3000, 1600, 40)])
+def test_keys_of_minus_infinity(dev, N, m, n):
+    # the oldest m entries have the logit -inf in every row: as if they were not in the list
+    import torch
+    s = Setup(dev, "bf16", "bf16", 1, 4, 1, 128, [N], n, seed=N + n)
+    s.k[0, s.live[:m].long(), 0, 0] = float("-inf")
+    q = s.queries(n)
+    q.view(-1, 128)[:, 0] = q.view(-1, 128)[:, 0].abs() + 0.5
+    out = s.run(q)
+    s.live, s.lengths, s.n_live = s.live[m:], [N - m], [N - m]
+    s.check(out, q, [n])
+
+
+@pytest.mark.parametrize("N,n", [(3, 2), (90, 90), (2000, 2)])
+def test_rows_of_minus_infinity_alone(dev, N, n):
+    # a softmax over nothing but -inf is NaN; a token that sees no entry at all stays zero
+    import torch
+    s = Setup(dev, "bf16", "bf16", 1, 4, 1, 64, [N], n, seed=N)
+    s.k[..., 0] = float("-inf")
+    q = s.queries(n)
+    q.view(-1, 64)[:, 0] = q.view(-1, 64)[:, 0].abs() + 0.5
+    assert s.run(q).isnan().all()
+    s.nl.fill_(1)
+    out = s.run(q).view(4, n, 64)
+    assert out[:, :n - 1].eq(0).all() and out[:, n - 1].isnan().all()
