@@ -347,6 +347,9 @@ def quant_load(cache: QuantPool, pool: Pool, sess: Sessions, src, dst=None, n_ro
 def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sinks: int, window: int, tokens: int, io,
             stream) -> None:
     import torch
+    for x, name in ((sinks, "sinks"), (window, "window")):      # a wider one would lose its high bits on the way
+        if not 0 <= x < 1 << 31:
+            raise IkvError(-1, func, f"{name} is {x}")
     numel = tokens * cache.L * cache.Hq * cache.D
     dt = torch.float32 if io == IKV_F32 else torch.bfloat16
     _tensor(q, dt, numel, func, "q")

@@ -165,3 +165,17 @@ def test_binding_checks_tensors():
         ikv.attend_chunk_quant(c, sess, q, live, n, q.clone(), ws)
     with pytest.raises(ikv.IkvError, match="not on a GPU"):
         ikv.quant_store(c, ikv.Pool(), sess, None, live)
+
+
+@pytest.mark.parametrize("kw", [dict(sinks=1 << 31), dict(window=(1 << 32) + 5), dict(sinks=-1), dict(window=-1 << 32)])
+def test_binding_checks_window(kw):
+    # past 32 bits they would arrive as other numbers
+    kc = torch.zeros(1, 4, 2, 64, dtype=torch.int8)
+    c = ikv.make_quant_pool(kc, kc, torch.zeros(1, 4, 2, 2), 1, 4, 2, 64, 4)
+    sess = ikv.Sessions([dict(slot_off=0, mem_off=0, qspan_off=0, qpos_off=0, N=3, pi=0, qs=1, qe=3, C=3,
+                              radix_prefix=0, R=1, nq=0)], "cpu")
+    live, n = torch.zeros(3, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    q = torch.zeros(1 * 4 * 2 * 64, dtype=torch.bfloat16)
+    for f in (ikv.attend_chunk_quant, ikv.decode_attend_quant):
+        with pytest.raises(ikv.IkvError, match="sinks is|window is"):
+            f(c, sess, q, live, n, q.clone(), ikv.Workspace("cpu"), **kw)
