@@ -100,7 +100,8 @@ class RetentionStep:
 
     def quantise(self, code: str = "int8"):
         """Put the rows of the live slots into an 8-bit cache of the pool's shape ("int8" or "e4m3"), same slots:
-        the decode over it reads half the bytes, and the pool can go."""
+        the decode over it reads half the bytes, and the pool can go. Of the rows as they are now: call it again
+        after each step that changes them."""
         import torch
         ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
         if getattr(self, "k_codes", None) is None or self.k_codes.dtype != ct:

@@ -14,7 +14,7 @@ def test_e4m3_table():
 
 
 def test_int8_by_hand():
-    # a = 2: scale 2/127; x = 1 is 63.5, a tie: 64 is even; -1 likewise; 0.5 is 31.75; 3/127 ties 1.5 * ... no: 127 * 3/127 / 2
+    # a = 2: scale 2/127; x = 1 is 63.5, a tie: 64 is even; -1 likewise; 0.5 is 31.75; 3/127 is 1.5 at float64's rounding
     c, s = qo.quantise(np.array([2.0, 1.0, -1.0, 0.5, 3.0 / 127, 0.0]), "int8")
     assert s == np.float32(2 / 127)
     assert list(c.view(np.int8)) == [127, 64, -64, 32, 2, 0]
