@@ -5,7 +5,8 @@
 // tokens are neighbours with nearly the same entries to see. Bound by the matrix cores and the
 // vector unit's work per logit together (busy 0.41 to 0.48 of the cycles, at a clock that falls
 // to 1.8 to 2.0 GHz under them): Qwen3-8B, 509 tokens over 8192 entries, 2.54 TFLOP: int8 2.70 ms,
-// E4M3 2.38; 14B, 1024 tokens, bf16, window 4096, 4.13 TFLOP: 4.06 ms. 256 rows: of 128, four
+// E4M3 2.38; 14B, 1024 tokens, bf16, window 4096, 4.13 TFLOP: 4.06 ms, on the fastest machine
+// (2.8 to 3.1 and 4.2 to 4.6 on others). 256 rows: of 128, four
 // waves, two workgroups a CU stage every tile twice as often (3.06 ms against 2.82); of 64 rows a
 // wave the registers spill (6.0 ms).
 //   staging   rows or codes go from HBM through registers, are made bf16 (exactly:
