@@ -9,6 +9,7 @@
 #include "decode_plan.hpp"
 #include "ikv.h"
 #include "ikv_error.hpp"
+#include "quant_rows.hpp"
 
 namespace ikv {
 
@@ -322,7 +323,6 @@ hipError_t launch_prefill(const ikv_pool &pool, const ikv_session *sess_dev, int
                           const int32_t *hist, const int32_t *n_hist, double base, float decay, float *M,
                           void *q_out, void *out, float *kq, float *ws, int64_t kq_floats, hipStream_t st);
 
-constexpr int QUANT_MOST = (1 << 24) - 1;  // rows of a session in one call: a workgroup or more each, under 2^32 threads
 hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
                               const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
 hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,

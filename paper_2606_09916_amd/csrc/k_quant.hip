@@ -13,13 +13,10 @@
 //         (ties missed by no less than 2^-33).
 //   e4m3  scale = 2^e with 448 2^e >= a > 224 2^e: x / scale is exact, and the conversion
 //         rounds once.
-#include <algorithm>
-
 #include "ikv_internal.hpp"
+#include "quant_rows.hpp"
 
 namespace ikv {
-
-constexpr int QT = 256;                          // threads per workgroup
 
 template <typename T> struct Row8;               // 8 channels as loaded
 template <> struct Row8<uint16_t> {
@@ -99,7 +96,6 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
 // many bytes in flight per CU. 8192 rows of 36 layers x 8 heads, D = 128, bf16, E4M3: stored in
 // 350 us (5.2 TB/s read and written), read back in 311 (5.9); with one place a thread both took
 // 1331, with eight 666.
-constexpr int QU = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool, const T *__restrict__ vpool,
@@ -113,7 +109,7 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
   const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
   const ikv_session s = sess[b];
   const int k0 = blockIdx.x * group;
-  const int todo = min(group, quant_rows(s, n_rows, b) - k0) * per;
+  const int todo = quant_places(group, quant_rows(s, n_rows, b), k0, per);
   const int64_t e0 = s.slot_off + k0;
   for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
     Row8<T> rk[QU], rv[QU];
@@ -193,7 +189,7 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
   const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
   const ikv_session s = sess[b];
   const int k0 = blockIdx.x * group;
-  const int todo = min(group, quant_rows(s, n_rows, b) - k0) * per;
+  const int todo = quant_places(group, quant_rows(s, n_rows, b), k0, per);
   const int64_t e0 = s.slot_off + k0;
   for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
     uint2 wk[QU], wv[QU];
@@ -225,8 +221,7 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
   }
 }
 
-// Entries of a workgroup: QU places per thread, one entry at least.
-static int quant_group(const ikv_quant_pool &c) { return std::max(1, QT * QU / (c.Hkv * (c.D / 8))); }
+static int quant_group(const ikv_quant_pool &c) { return quant_group(c.Hkv * (c.D / 8)); }
 static dim3 quant_grid(const ikv_quant_pool &c, int B, int maxN) {
   return dim3(unsigned(cdiv(maxN, quant_group(c))), unsigned(c.L), unsigned(B));
 }
