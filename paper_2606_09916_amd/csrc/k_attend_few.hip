@@ -265,14 +265,20 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
           }
         split_parts<PP>(pw, pf[k]);
       }
-      if constexpr (FMT == KV_BF16) {
+      if constexpr (FMT != KV_INT8) {
         if (!whole) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
 #pragma unroll
             for (int k = 0; k < VW; ++k) {
-              odd |= odd_low(x.v[e][k]) | odd_high(x.v[e][k]);
-              x.v[e][k] = bf16_finite(x.v[e][k]);
+              if constexpr (FMT == KV_BF16) {
+                odd |= odd_low(x.v[e][k]) | odd_high(x.v[e][k]);
+                x.v[e][k] = bf16_finite(x.v[e][k]);
+              } else {
+                const uint32_t nans = e4m3_nans(x.v[e][k]);
+                odd |= nans != 0;
+                x.v[e][k] = e4m3_finite(x.v[e][k], nans);
+              }
             }
         }
       }
@@ -326,11 +332,11 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         compute(x[u], at);
       }
     }
-    if constexpr (FMT == KV_BF16) {
+    if constexpr (FMT != KV_INT8) {
       if (__builtin_amdgcn_ballot_w64(odd) != 0)
         for (int v = v0; v < v1; ++v) {
           const int e = v < first ? v : v + gap;
-          const uint16_t *row = reinterpret_cast<const uint16_t *>(vbase + row_at(list[e], 0));
+          const char *row = vbase + row_at(list[e], 0);
 #pragma unroll
           for (int k = 0; k < NR; ++k) {
             const bool see = (e <= own[k]) & ((a.window == 0) | (e < a.sinks) | (e > own[k] - a.window));
@@ -338,8 +344,13 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int j = 0; j < NC; ++j) {
-                const uint16_t y = row[NC * (4 * g + i) + j];
-                o[k][j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+                const int ch = NC * (4 * g + i) + j;
+                if constexpr (FMT == KV_BF16) {
+                  const uint16_t y = reinterpret_cast<const uint16_t *>(row)[ch];
+                  o[k][j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+                } else {
+                  o[k][j][i] += see && (row[ch] & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+                }
               }
           }
         }

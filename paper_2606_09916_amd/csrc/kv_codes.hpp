@@ -57,5 +57,9 @@ __device__ __forceinline__ bool odd_high(uint32_t w) { return (w & 0x7f800000u) 
 __device__ __forceinline__ uint32_t bf16_finite(uint32_t w) {
   return (odd_low(w) ? 0u : w & 0xffffu) | (odd_high(w) ? 0u : w & 0xffff0000u);
 }
+// The same for 4 E4M3 codes of a word, whose only value that is not finite is NaN, 0x7f and 0xff:
+// 0x80 in each such byte. (0x7f + 1 stays within its byte.)
+__device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t e4m3_finite(uint32_t w, uint32_t nans) { return w & ~(nans | (nans - (nans >> 7))); }
 
 }  // namespace ikv
