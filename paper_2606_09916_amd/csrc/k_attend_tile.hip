@@ -217,9 +217,13 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
           y[0] = e4m3_scaled4(x.x, scale), y[1] = e4m3_scaled4(x.y, scale);
           y[2] = e4m3_scaled4(x.z, scale), y[3] = e4m3_scaled4(x.w, scale);
           const bool bad = !(scale < INFINITY);
-          if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) {
-            odd |= look;
-            y[0] = y[1] = y[2] = y[3] = look ? make_uint2(0u, 0u) : make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+          if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) y[0] = y[1] = y[2] = y[3] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+          if (look) {                              // NaN codes and scales, products past the largest bf16
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              odd |= odd_low(y[i].x) | odd_high(y[i].x) | odd_low(y[i].y) | odd_high(y[i].y);
+              y[i] = make_uint2(bf16_finite(y[i].x), bf16_finite(y[i].y));
+            }
           }
         } else {
           y[0] = codes4<FMT>(x.x), y[1] = codes4<FMT>(x.y), y[2] = codes4<FMT>(x.z), y[3] = codes4<FMT>(x.w);
@@ -423,6 +427,22 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
             for (int k = 0; k < 16; ++k) {
               const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
               o[db][k] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+            }
+        } else if constexpr (FMT == KV_E4M3) {
+          const Off at = row_at(list[j]);
+          const float scale = scale_at(at).y;
+          const bool bad = !(scale < INFINITY);
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+              const uint2 y = e4m3_scaled4(*reinterpret_cast<const uint32_t *>(vbase + at + (32 * db + 8 * i4 + 4 * h2)), scale);
+              const uint32_t z[4] = {y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float x = bad ? __uint_as_float(0x7fc00000u) : odd_high(z[i]) ? __uint_as_float(z[i]) : 0.f;
+                o[db][4 * i4 + i] += see ? x : 0.f;
+              }
             }
         } else {
           const float add = see && !(scale_at(row_at(list[j])).y < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;

@@ -1,5 +1,6 @@
 """Rows of the 8-bit cache that a token does not see add nothing to it, whatever bytes
-they hold, E4M3's NaN codes among them. Tokens that see such a value row get what it stands for.
+they hold: E4M3's NaN codes, and codes whose product with the scale passes the largest float.
+Tokens that see such a value row get what it stands for.
 
 Outputs of the tokens that see no changed row, and channels whose values did not change, have to
 be the bytes of the run before the change: a row's own weights and sums do not depend on it."""
@@ -14,6 +15,9 @@ SINKS, WINDOW = 2, 20
 # (KV heads, heads per KV head, D, tokens) that one wave takes as one 16-row block, or two
 FEW = [(2, 2, 128, 1), (2, 2, 128, 6), (1, 4, 64, 3)]
 FEW_2 = [(2, 2, 128, 13), (1, 8, 64, 4)]
+# blocks of 128 and of 256 rows
+TILES = [(2, 2, 128, 50), (1, 4, 64, 30), (2, 2, 128, 140), (1, 4, 64, 300)]
+FORMS = [(io, f) for io in ("bf16", "f32") for f in FEW + FEW_2 + TILES]
 
 
 def _changed(N, n):
@@ -37,7 +41,7 @@ def _runs(dev, code, io, form, change, N=500):
     return clean, run(), sees
 
 
-@pytest.mark.parametrize("io,form", [(io, f) for io in ("bf16", "f32") for f in FEW] + [("bf16", f) for f in FEW_2])
+@pytest.mark.parametrize("io,form", FORMS)
 @pytest.mark.parametrize("byte", [0x7f, 0xff])
 def test_nan_codes(dev, io, form, byte):
     import torch
@@ -56,3 +60,22 @@ def test_nan_codes(dev, io, form, byte):
     spoiled[chan] = True
     assert out[:, sees][..., spoiled].isnan().all()
     assert torch.equal(out[:, sees][..., ~spoiled], clean[:, sees][..., ~spoiled])
+
+
+@pytest.mark.parametrize("io,form", FORMS)
+def test_codes_past_the_largest_float(dev, io, form):
+    # 256 * 2^120, as the store itself writes the top of the range, and 448 * 2^127
+    import torch
+
+    def change(s, hidden, some):
+        for x, i in ((s.k, 0), (s.v, 1)):
+            x.view(torch.uint8)[:, hidden] = 0x78
+            s.sc[:, hidden, :, i] = 2.0 ** 120
+            x.view(torch.uint8)[:, hidden[::2]] = 0xfe
+            s.sc[:, hidden[::2], :, i] = 2.0 ** 127
+        s.v.view(torch.uint8)[:, some] = 0x78
+        s.sc[:, some, :, 1] = 2.0 ** 120
+
+    clean, out, sees = _runs(dev, "e4m3", io, form, change)
+    assert torch.equal(out[:, ~sees], clean[:, ~sees])
+    assert not (out[:, sees].abs() < 2.0 ** 100).any()
