@@ -216,7 +216,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         if constexpr (FMT == KV_E4M3) {
           y[0] = e4m3_scaled4(x.x, scale), y[1] = e4m3_scaled4(x.y, scale);
           y[2] = e4m3_scaled4(x.z, scale), y[3] = e4m3_scaled4(x.w, scale);
-          const bool bad = !(scale < INFINITY);
+          const bool bad = !(fabsf(scale) < INFINITY);
           if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) y[0] = y[1] = y[2] = y[3] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
           if (look) {                              // NaN codes and scales, products past the largest bf16
 #pragma unroll
@@ -244,7 +244,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       }
       if constexpr (FMT == KV_INT8) {
         if (tid < TILE_KEYS) {
-          const bool bad = look && !(r.sc.y < INFINITY);
+          const bool bad = look && !(fabsf(r.sc.y) < INFINITY);
           odd |= bad;
           sc_[par][0][tid] = r.sc.x * to_log2;
           sc_[par][1][tid] = bad ? 0.f : r.sc.y;
@@ -431,7 +431,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         } else if constexpr (FMT == KV_E4M3) {
           const Off at = row_at(list[j]);
           const float scale = scale_at(at).y;
-          const bool bad = !(scale < INFINITY);
+          const bool bad = !(fabsf(scale) < INFINITY);
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -445,7 +445,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
               }
             }
         } else {
-          const float add = see && !(scale_at(row_at(list[j])).y < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;
+          const float add = see && !(fabsf(scale_at(row_at(list[j])).y) < INFINITY) ? __uint_as_float(0x7fc00000u) : 0.f;
 #pragma unroll
           for (int db = 0; db < DB; ++db) o[db] += add;
         }

@@ -1,6 +1,7 @@
 """Rows of the 8-bit cache that a token does not see add nothing to it, whatever bytes
-they hold: E4M3's NaN codes, and codes whose product with the scale passes the largest float.
-Tokens that see such a value row get what it stands for.
+and scales they hold: E4M3's NaN codes, codes whose product with the scale passes the largest
+float, scales that are infinite of either sign. Tokens that see such a value row get what it
+stands for.
 
 Outputs of the tokens that see no changed row, and channels whose values did not change, have to
 be the bytes of the run before the change: a row's own weights and sums do not depend on it."""
@@ -79,3 +80,18 @@ def test_codes_past_the_largest_float(dev, io, form):
     clean, out, sees = _runs(dev, "e4m3", io, form, change)
     assert torch.equal(out[:, ~sees], clean[:, ~sees])
     assert not (out[:, sees].abs() < 2.0 ** 100).any()
+
+
+@pytest.mark.parametrize("io,form", FORMS)
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("scale", [float("-inf"), float("inf"), float("nan")])
+def test_scales_that_are_not_finite(dev, code, io, form, scale):
+    import torch
+
+    def change(s, hidden, some):
+        s.sc[:, hidden] = scale
+        s.sc[:, some, :, 1] = scale
+
+    clean, out, sees = _runs(dev, code, io, form, change)
+    assert torch.equal(out[:, ~sees], clean[:, ~sees])
+    assert not torch.isfinite(out[:, sees]).any()
