@@ -470,8 +470,8 @@ typedef struct ikv_quant_pool {
  *        are not listed stay as they are.
  *   n_rows: device int32 [B], or NULL: N rows per session; values are clamped to [0, N].
  * pool and cache must agree in L, Hkv and D (IKV_ESHAPE); the pool's rows are bf16 or
- * float32, 16-byte aligned. At most 2^24 - 1 rows per session, 65535 sessions and layers
- * (IKV_EUNSUPPORTED). Needs no workspace. Only N and slot_off of the sessions are read.
+ * float32, 16-byte aligned. At most 2^24 - 1 rows per session, 65535 sessions, layers and KV
+ * heads (IKV_EUNSUPPORTED). Needs no workspace. Only N and slot_off of the sessions are read.
  */
 ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool,
                            const ikv_session *sess, const ikv_session *sess_dev, int32_t B,

@@ -330,8 +330,8 @@ ikv_status check_quant_rows(const ikv_quant_pool *c, const ikv_pool *p, const ik
   if ((reinterpret_cast<uintptr_t>(p->k_pool) | reinterpret_cast<uintptr_t>(p->v_pool)) % 16)
     return fail(IKV_EINVAL, "pool: k_pool and v_pool must be 16-byte aligned");
   if ((r = check_sessions(sess, sess_dev, B))) return r;
-  if (B > 65535 || c->L > 65535 || max_n(sess, B) > ikv::QUANT_MOST)
-    return fail(IKV_EUNSUPPORTED, "more than 65535 sessions or layers, or %d rows of a session", ikv::QUANT_MOST);
+  if (B > 65535 || c->L > 65535 || c->Hkv > 65535 || max_n(sess, B) > ikv::QUANT_MOST)
+    return fail(IKV_EUNSUPPORTED, "more than 65535 sessions, layers or KV heads, or %d rows of a session", ikv::QUANT_MOST);
   if (B > 0 && !cache_ids) return fail(IKV_EINVAL, "%s is NULL", cache_what);
   if (!pool_ids)
     for (int b = 0; b < B; ++b)
