@@ -137,8 +137,11 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     sum += len;
     most = std::max<int64_t>(most, sess[b].N);
   }
-  p.few = int64_t(p.max_n) * G <= (a.format != KV_BF16 && !a.io_f32 ? 2 * FEW_ROWS : FEW_ROWS);
   p.splits = p.blocks = 1;
+  // launch grids: 65535 in y and z; entries and rows stay below 2^30 (and the products here in 64 bits)
+  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || most > ATTEND_MOST || int64_t(p.max_n) * G > ATTEND_MOST;
+  if (p.too_large) return p;
+  p.few = int64_t(p.max_n) * G <= (a.format != KV_BF16 && !a.io_f32 ? 2 * FEW_ROWS : FEW_ROWS);
   const int64_t groups = std::max<int64_t>(1, int64_t(a.L) * B);
   if (p.few) {
     p.rows = p.max_n * G;
@@ -152,10 +155,9 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
   // the workspace is sized without the window
   if (window) p.splits = std::min(p.splits, attend_plan(a, sess, B, decode, 0, 0).splits);
   if (p.splits > 1) p.ws_floats = int64_t(B) * a.L * a.Hkv * p.blocks * p.splits * p.rows * (a.D + 2);
-  // launch grids: 65535 in y and z, under 2^32 threads in x; entries and rows stay below 2^30
-  const int64_t threads = (groups * a.Hkv + 7) / 8 * 8 * p.blocks * p.splits * 2 * p.rows;
-  p.too_large = B > 65535 || int64_t(a.L) * a.Hq > 65535 || most > ATTEND_MOST || int64_t(p.max_n) * G > ATTEND_MOST ||
-                (!p.few && threads >= int64_t(1) << 32);
+  // under 2^32 threads in x
+  const int64_t wgs = (groups * a.Hkv + 7) / 8 * 8 * p.blocks * p.splits;
+  p.too_large = !p.few && wgs >= (int64_t(1) << 32) / (2 * p.rows);
   return p;
 }
 
