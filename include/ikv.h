@@ -466,8 +466,8 @@ typedef struct ikv_quant_pool {
  * kept rows of a retention event (src = dst = the live list), a change of slots.
  *   src: device int32 per session [N], or NULL: row slot_off + k of the pool.
  *   dst: device int32 per session [N]; entries equal to cache->dead_slot are skipped (the
- *        padding of a batch). A slot may be listed once only in a call; rows of slots that
- *        are not listed stay as they are.
+ *        padding of a batch), whatever src holds there. A slot may be listed once only in a
+ *        call; rows of slots that are not listed stay as they are.
  *   n_rows: device int32 [B], or NULL: N rows per session; values are clamped to [0, N].
  * pool and cache must agree in L, Hkv and D (IKV_ESHAPE); the pool's rows are bf16 or
  * float32, 16-byte aligned. At most 2^24 - 1 rows per session, 65535 sessions, layers and KV

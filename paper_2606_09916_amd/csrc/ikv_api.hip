@@ -230,15 +230,19 @@ ikv_status debug_fetch(std::vector<T> &h, const T *dev, int64_t n, hipStream_t s
   return IKV_OK;
 }
 
+ikv_status debug_id(int32_t id, int64_t i, int64_t lo, int64_t hi, const char *what, int b) {
+  if (id >= lo && id < hi) return IKV_OK;
+  return fail(IKV_EINVAL, "IKV_DEBUG: session %d: %s[%lld] = %d outside [%lld, %lld)", b, what, (long long)i, id,
+              (long long)lo, (long long)hi);
+}
+
 // Entries [off, off + n) of the device array `ids` must lie in [lo, hi).
 ikv_status debug_ids(const int32_t *ids, int64_t off, int64_t n, int64_t lo, int64_t hi, hipStream_t st,
                      const char *what, int b) {
   std::vector<int32_t> h;
   if (ikv_status r = debug_fetch(h, ids + off, n, st, what, b)) return r;
   for (int64_t i = 0; i < n; ++i)
-    if (h[size_t(i)] < lo || h[size_t(i)] >= hi)
-      return fail(IKV_EINVAL, "IKV_DEBUG: session %d: %s[%lld] = %d outside [%lld, %lld)", b, what, (long long)i,
-                  h[size_t(i)], (long long)lo, (long long)hi);
+    if (ikv_status r = debug_id(h[size_t(i)], i, lo, hi, what, b)) return r;
   return IKV_OK;
 }
 
@@ -261,8 +265,8 @@ ikv_status debug_live(const ikv_session *sess, int B, const int32_t *live, const
   return IKV_OK;
 }
 
-// The slot lists of a store into, or a load from, the 8-bit cache: ids in range, and no
-// destination listed twice among the entries that are not skipped.
+// The slot lists of a store into, or a load from, the 8-bit cache, among the entries that are not
+// skipped: ids in range, and no destination listed twice.
 ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache_ids, int64_t cache_slots,
                             const char *cache_what, int32_t dead, const int32_t *pool_ids, int64_t pool_slots,
                             const char *pool_what, bool to_cache, const int32_t *n_rows, hipStream_t st) {
@@ -271,15 +275,16 @@ ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache
     int64_t n = sess[b].N;
     if (n_rows)
       if (ikv_status r = debug_count(n_rows, b, n, st, "n_rows", &n)) return r;
-    if (ikv_status r = debug_ids(cache_ids, sess[b].slot_off, n, 0, cache_slots, st, cache_what, b)) return r;
-    if (pool_ids)
-      if (ikv_status r = debug_ids(pool_ids, sess[b].slot_off, n, 0, pool_slots, st, pool_what, b)) return r;
     if (ikv_status r = debug_fetch(h, cache_ids + sess[b].slot_off, n, st, cache_what, b)) return r;
-    if (!to_cache && pool_ids)
+    if (pool_ids)
       if (ikv_status r = debug_fetch(hp, pool_ids + sess[b].slot_off, n, st, pool_what, b)) return r;
-    for (int64_t k = 0; k < n; ++k)
-      if (h[size_t(k)] != dead)
-        written.push_back(to_cache ? h[size_t(k)] : pool_ids ? hp[size_t(k)] : int32_t(sess[b].slot_off + k));
+    for (int64_t k = 0; k < n; ++k) {
+      const int32_t c = h[size_t(k)], q = pool_ids ? hp[size_t(k)] : int32_t(sess[b].slot_off + k);
+      if (ikv_status r = debug_id(c, k, 0, cache_slots, cache_what, b)) return r;
+      if (c == dead) continue;                     // skipped: its pool id is not read
+      if (ikv_status r = debug_id(q, k, 0, pool_slots, pool_what, b)) return r;
+      written.push_back(to_cache ? c : q);
+    }
   }
   std::sort(written.begin(), written.end());
   const auto twice = std::adjacent_find(written.begin(), written.end());
