@@ -441,8 +441,11 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *             one: the code does not depend on the precision it is computed in);
  *   IKV_E4M3  scale = the least power of two with 448 scale >= a, code_d = x_d / scale
  *             rounded to the nearest E4M3 value, ties to even. A power of two costs a
- *             floating code no precision, and makes reading back exact, in bf16 too; the
- *             calls take the scales of E4M3 rows as powers of two, whoever wrote them.
+ *             floating code no precision, and makes reading back exact, in bf16 too. The
+ *             attention calls take the scales of E4M3 rows as normal powers of two, or NaN,
+ *             whoever wrote them: with any other their results are not defined (the chunk
+ *             call uses the power below it). With IKV_DEBUG=1 they refuse one that a token
+ *             sees.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
  * every channel. L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
  * of a larger cache is a descriptor with L = 1 and pointers to that layer.
