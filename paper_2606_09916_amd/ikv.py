@@ -147,11 +147,11 @@ def _tensor(t, dtype, numel: int, func: str, name: str) -> None:
 
 
 def _place(func: str, sess, stream, *tensors) -> int:
-    """The stream to enqueue on, once every tensor is on its device."""
+    """The stream to enqueue on, once every tensor is on its device, and every descriptor's tensors are."""
     import torch
     dev = sess.dev.device
     for t in tensors:
-        if t is not None and t.device != dev:
+        if t is not None and getattr(t, "device", dev) != dev:    # a descriptor filled in by hand has none
             raise IkvError(-1, func, "tensors and sessions on different devices")
     if dev.type != "cuda":
         raise IkvError(-1, func, f"sessions are on {dev}, not on a GPU")
@@ -167,7 +167,9 @@ def make_pool(k_pool, v_pool, L, Hq, Hkv, D, num_slots, dead_slot=0) -> Pool:
     """Pool descriptor over two device tensors [L][num_slots][Hkv][D] (bfloat16 or float32)."""
     import torch
     dt = {torch.bfloat16: IKV_BF16, torch.float32: IKV_F32}[k_pool.dtype]
-    return Pool(L, Hq, Hkv, D, num_slots, dead_slot, dt, k_pool.data_ptr(), v_pool.data_ptr())
+    p = Pool(L, Hq, Hkv, D, num_slots, dead_slot, dt, k_pool.data_ptr(), v_pool.data_ptr())
+    p.device = k_pool.device
+    return p
 
 
 def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slot=0, io_dtype=None) -> QuantPool:
@@ -186,8 +188,12 @@ def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slo
     _tensor(k_codes, k_codes.dtype, rows * D, what, "k_codes")
     _tensor(v_codes, k_codes.dtype, rows * D, what, "v_codes")
     _tensor(scales, torch.float32, rows * 2, what, "scales")
-    return QuantPool(L, Hq, Hkv, D, num_slots, dead_slot, code, io, 0, k_codes.data_ptr(), v_codes.data_ptr(),
-                     scales.data_ptr())
+    if not k_codes.device == v_codes.device == scales.device:
+        raise IkvError(-1, what, "codes and scales on different devices")
+    c = QuantPool(L, Hq, Hkv, D, num_slots, dead_slot, code, io, 0, k_codes.data_ptr(), v_codes.data_ptr(),
+                  scales.data_ptr())
+    c.device = k_codes.device
+    return c
 
 
 class Sessions:
@@ -331,7 +337,7 @@ def _lists(sess: Sessions, ids, counts, func: str, names) -> None:
 def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=None, stream=None) -> None:
     """Quantise rows of a pool into the 8-bit cache: slot src[k] (None: row slot_off + k) of the pool to slot dst[k]."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_store", ("src", "dst"))
-    st = _place("ikv_quant_store", sess, stream, src, dst, n_rows)
+    st = _place("ikv_quant_store", sess, stream, cache, pool, src, dst, n_rows)
     _check(lib().ikv_quant_store(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
                                  _ptr(dst), _ptr(n_rows), st), "ikv_quant_store")
 
@@ -339,13 +345,13 @@ def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=N
 def quant_load(cache: QuantPool, pool: Pool, sess: Sessions, src, dst=None, n_rows=None, stream=None) -> None:
     """Read rows of the 8-bit cache back: slot src[k] of the cache to slot dst[k] (None: row slot_off + k) of the pool."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_load", ("src", "dst"))
-    st = _place("ikv_quant_load", sess, stream, src, dst, n_rows)
+    st = _place("ikv_quant_load", sess, stream, cache, pool, src, dst, n_rows)
     _check(lib().ikv_quant_load(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
                                 _ptr(dst), _ptr(n_rows), st), "ikv_quant_load")
 
 
-def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sinks: int, window: int, tokens: int, io,
-            stream) -> None:
+def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, ws: Workspace, need: int, sinks: int, window: int,
+            tokens: int, io, stream) -> None:
     import torch
     for x, name in ((sinks, "sinks"), (window, "window")):      # a wider one would lose its high bits on the way
         if not 0 <= x < 1 << 31:
@@ -355,7 +361,8 @@ def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sink
     _tensor(q, dt, numel, func, "q")
     _tensor(out, dt, numel, func, "out")
     _lists(sess, (live,), n_live, func, ("live",))
-    st = _place(func, sess, stream, q, out, live, n_live)
+    wp, wn = ws.get(need)
+    st = _place(func, sess, stream, cache, q, out, live, n_live, ws.buf if wn else None)
     _check(getattr(lib(), func)(ctypes.byref(cache), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(q), _ptr(live),
                                 _ptr(n_live), sinks, window, _ptr(out), wp, wn, st), func)
 
@@ -363,25 +370,22 @@ def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, wp, wn, sink
 def decode_attend_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
                         window: int = 0, stream=None) -> None:
     """One new token per session over the 8-bit cache: q, out [B][L][Hq][D] of the cache's io_dtype."""
-    wp, wn = ws.get(quant_workspace_bytes(cache, sess, CALL_DECODE))
-    _attend("ikv_decode_attend_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, sess.B, cache.io_dtype,
-            stream)
+    _attend("ikv_decode_attend_quant", cache, sess, q, live, n_live, out, ws, quant_workspace_bytes(cache, sess, CALL_DECODE),
+            sinks, window, sess.B, cache.io_dtype, stream)
 
 
 def attend_chunk(pool: Pool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0, window: int = 0,
                  stream=None) -> None:
     """The newest qe - qs tokens of each session over a bf16 pool: q, out packed by session, [L][Hq][n][D]."""
-    wp, wn = ws.get(workspace_bytes(pool, sess, CALL_CHUNK))
-    _attend("ikv_attend_chunk", pool, sess, q, live, n_live, out, wp, wn, sinks, window, sess.span_tokens, IKV_BF16,
-            stream)
+    _attend("ikv_attend_chunk", pool, sess, q, live, n_live, out, ws, workspace_bytes(pool, sess, CALL_CHUNK), sinks, window,
+            sess.span_tokens, IKV_BF16, stream)
 
 
 def attend_chunk_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
                        window: int = 0, stream=None) -> None:
     """attend_chunk over the 8-bit cache: q, out of the cache's io_dtype."""
-    wp, wn = ws.get(quant_workspace_bytes(cache, sess, CALL_CHUNK))
-    _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, wp, wn, sinks, window, sess.span_tokens,
-            cache.io_dtype, stream)
+    _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, ws, quant_workspace_bytes(cache, sess, CALL_CHUNK),
+            sinks, window, sess.span_tokens, cache.io_dtype, stream)
 
 
 # ----------------------------------------------------------------------------- timing
