@@ -70,6 +70,7 @@ class RetentionStep:
         self.n_live = torch.empty(self.B, dtype=torch.int32, device=device)
         self.out = torch.empty_like(self.q_dec)
         self.ws = ikv.Workspace(device)
+        self.cache = None                        # the 8-bit cache, made by quantise()
 
     # ---------------------------------------------------------------- calls
     def reset(self):
@@ -103,8 +104,10 @@ class RetentionStep:
         the decode over it reads half the bytes, and the pool can go. Of the rows as they are now: call it again
         after each step that changes them."""
         import torch
-        ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
-        if getattr(self, "k_codes", None) is None or self.k_codes.dtype != ct:
+        ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}.get(code)
+        if ct is None:
+            raise ikv.IkvError(-1, "RetentionStep.quantise", f"code {code!r} (\"int8\" or \"e4m3\")")
+        if self.cache is None or self.k_codes.dtype != ct:
             shape = (self.L, self.num_slots, self.Hkv, self.D)
             self.k_codes, self.v_codes = (torch.empty(shape, dtype=ct, device=self.device) for _ in range(2))
             self.code_scales = torch.empty((*shape[:3], 2), dtype=torch.float32, device=self.device)
@@ -113,6 +116,9 @@ class RetentionStep:
         ikv.quant_store(self.cache, self.pool, self.sess, self.live, self.live, self.n_live)
 
     def decode_quant(self, sinks: int = 0, window: int = 0):
+        """The decode over the 8-bit cache that ``quantise`` filled."""
+        if self.cache is None:
+            raise ikv.IkvError(-1, "RetentionStep.decode_quant", "no 8-bit cache yet: call quantise() first")
         ikv.decode_attend_quant(self.cache, self.sess, self.q_dec, self.live, self.n_live, self.out, self.ws,
                                 sinks=sinks, window=window)
 
