@@ -218,7 +218,9 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
           y[2] = e4m3_scaled4(x.z, scale), y[3] = e4m3_scaled4(x.w, scale);
           const bool bad = !(fabsf(scale) < INFINITY);
           if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) y[0] = y[1] = y[2] = y[3] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
-          if (look) {                              // NaN codes and scales, products past the largest bf16
+          // NaN codes, products past the largest bf16 (448 * 2^119 is below it), scales that are not finite
+          if (look && __builtin_amdgcn_ballot_w64((e4m3_nans(x.x) | e4m3_nans(x.y) | e4m3_nans(x.z) | e4m3_nans(x.w)) != 0 ||
+                                                  !(fabsf(scale) < 0x1p120f)) != 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               odd |= odd_low(y[i].x) | odd_high(y[i].x) | odd_low(y[i].y) | odd_high(y[i].y);
@@ -415,7 +417,9 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       iterate(sB, sA, tile + 1, 1, r, oa, ob);
       __syncthreads();
     }
-    if (__syncthreads_or(odd))
+    // (the hint keeps E4M3's out of the loop's registers: 8 float32 layers, 20 tokens over 4000: 83 us, 87 without)
+    const bool again = __syncthreads_or(odd);
+    if (FMT == KV_E4M3 ? __builtin_expect(again, false) : again)
       for (int v = tb * TILE_KEYS; v < min(T, te * TILE_KEYS); ++v) {
         const int j = v < first ? v : v + gap;
         const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
