@@ -46,7 +46,8 @@
  *    attend_chunk, attend_chunk_quant) first copy them to the host, after the
  *    stream's earlier work, and return IKV_EINVAL naming the session, the array
  *    and the index of the first bad entry, with no kernel launched. This
- *    synchronises the stream on every call; it is meant for debugging.
+ *    synchronises the stream on every call; it is meant for debugging. The
+ *    attention calls on the 8-bit cache look at E4M3 scales too (ikv_quant_pool).
  */
 #ifndef IKV_H
 #define IKV_H
@@ -447,7 +448,8 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *             call uses the power below it). With IKV_DEBUG=1 they refuse one that a token
  *             sees.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
- * every channel. L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
+ * every channel. At the top of the range code * scale may round past the largest float and
+ * stand for an infinity (E4M3: channels from 248 * 2^120 on). L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
  * of a larger cache is a descriptor with L = 1 and pointers to that layer.
  */
 typedef struct ikv_quant_pool {
@@ -506,8 +508,13 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
  *     entries of the list, so positions that a retention event dropped take no room in the
  *     window. A token with i < 0 (a list shorter than its chunk) sees nothing and its output
  *     is zero. sinks and window are >= 0; window 0 means none, and sinks is then ignored.
- *   out = softmax_j(q . K_j / sqrt(D)) . V_j over the entries seen, softmax and sums in
- *     float32. Entries a token does not see add nothing to it, whatever their rows hold.
+ *   out = softmax_j(q . K_j / sqrt(D)) . V_j over the entries seen, logits, softmax statistics
+ *     and sums in float32 (of weights up to 2^8 before they are divided). The weights enter the
+ *     product with V in bf16 parts: three for float32 outputs (each weight off by 2^-25 of it);
+ *     for bf16 outputs two (2^-17) where a KV head has up to 16 query rows (tokens times
+ *     Hq / Hkv; 32 over the 8-bit cache), and one (2^-8, to nearest; their sum is of the unrounded
+ *     ones) for longer chunks. Entries a token does not see add nothing to it, whatever their
+ *     rows and scales hold.
  *   q, out: device, 16-byte aligned, packed by session (session b's rows start after those of
  *     the sessions before it), [L][Hq][n][D] each: [B][L][Hq][D] for the decode. Their type is
  *     io_dtype of the cache, or bf16 for ikv_attend_chunk, which needs a bf16 pool

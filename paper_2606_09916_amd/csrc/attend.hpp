@@ -107,8 +107,9 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
 
 // Splits of the tile kernel, whose state is up to 256 rows of a split and worth only idle CUs
 // (us, Qwen3-8B's heads, n new tokens over 8701 int8 entries):
-//  - less than a round of workgroups: as many splits as fill one, of at least 256 entries. One
-//    layer, n = 509: 1 split 275, 4 111, 8 120; n = 64: 1 275, 24 36, 48 49.
+//  - less than a round of workgroups: as many splits as stay within one, of at least 256 entries.
+//    One layer, n = 509: 1 split 275, 4 111, 8 120; n = 64: 1 275, 24 36, 48 49. (From 129 to 255
+//    workgroups that is one; what more would give there has not been measured.)
 //  - one block of rows per head (mostly reading, and the state is small): of at least 1024
 //    entries, five rounds for 128 rows (36 layers, n = 20: 333 with one split, 275 with three, 265
 //    with five, 270 with eight), or the fewest that fill their rounds to 80% for 256 (n = 64: 616

@@ -6,7 +6,7 @@
 // vector unit's work per logit together (busy 0.41 to 0.48 of the cycles, at a clock that falls
 // to 1.8 to 2.0 GHz under them): Qwen3-8B, 509 tokens over 8192 entries, 2.54 TFLOP: int8 2.70 ms,
 // E4M3 2.38; 14B, 1024 tokens, bf16, window 4096, 4.13 TFLOP: 4.06 ms, on the fastest machine
-// (2.8 to 3.1 and 4.2 to 4.6 on others). 256 rows: of 128, four
+// (2.8 to 3.1, 2.4 to 2.55 and 4.2 to 4.6 on others). 256 rows: of 128, four
 // waves, two workgroups a CU stage every tile twice as often (3.06 ms against 2.82); of 64 rows a
 // wave the registers spill (6.0 ms).
 //   staging   rows or codes go from HBM through registers, are made bf16 (exactly:
@@ -21,8 +21,11 @@
 //             operand as they are; the transposing LDS reads (4 entries x 16 channels by 16
 //             lanes) bring the value operand in that order from row-major tiles.
 // Weights are rounded to bf16 for bf16 outputs (2^-8 each, no more than the output's own
-// rounding, and averaged over the entries; their sum is of the unrounded ones). float32
-// outputs take queries and weights as three bf16 parts.
+// rounding, and averaged over the entries; their sum is of the unrounded ones): against float64
+// the long chunks are off by 0.0018 to 0.0019 where the output's rounding alone is 0.0017. float32
+// outputs take queries and weights as three bf16 parts, which at D = 128 do not fit the
+// registers: 42 to 67 of a lane's are spilled (8 layers, 200 tokens over 4000: 348 to 377 us). Of the
+// bf16 outputs' instances, int8 with eight waves, and bf16 rows and E4M3 with four, spill two.
 #include <math.h>
 
 #include <type_traits>
@@ -200,7 +203,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       return !(vb < T && jb <= o0 && (a.window == 0 || jb < a.sinks || ja > o1 - a.window));
     };
     // the values and scales of `tile` (buffer tile & 1) and the keys of tile + 1. A value that is
-    // not finite would turn the zero weights of rows that do not see it into NaN: in a tile that
+    // not finite (a bf16 one, a NaN code, a scale, a product of both) would turn the zero weights of rows that do not see it into NaN: in a tile that
     // some row does not see whole it is left out and added after the loop.
     bool odd = false;
     auto put = [&](uint16_t *dst, uint4 x, float scale, bool look) __attribute__((always_inline)) {

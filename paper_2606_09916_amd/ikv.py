@@ -173,7 +173,7 @@ def make_pool(k_pool, v_pool, L, Hq, Hkv, D, num_slots, dead_slot=0) -> Pool:
 
 
 def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slot=0, io_dtype=None) -> QuantPool:
-    """8-bit cache descriptor over device tensors: codes [L][num_slots][Hkv][D] (int8 or float8_e4m3fn), scales
+    """8-bit cache descriptor over device tensors, which the caller keeps: codes [L][num_slots][Hkv][D] (int8 or float8_e4m3fn), scales
     [L][num_slots][Hkv][2] float32 (K's, V's). io_dtype: q and out of the attention calls, bfloat16 (the default) or
     float32."""
     import torch
@@ -197,7 +197,8 @@ def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slo
 
 
 class Sessions:
-    """Host array of session descriptors plus its device copy (same bytes)."""
+    """Host array of session descriptors plus its device copy (same bytes). Fixed once made: the copy, and the sizes that
+    the calls check their tensors against, are taken here; other rows need another object."""
 
     def __init__(self, rows, device):
         import torch
