@@ -46,8 +46,7 @@
  *    attend_chunk, attend_chunk_quant) first copy them to the host, after the
  *    stream's earlier work, and return IKV_EINVAL naming the session, the array
  *    and the index of the first bad entry, with no kernel launched. This
- *    synchronises the stream on every call; it is meant for debugging. The
- *    attention calls on the 8-bit cache look at E4M3 scales too (ikv_quant_pool).
+ *    synchronises the stream on every call; it is meant for debugging.
  */
 #ifndef IKV_H
 #define IKV_H
@@ -443,14 +442,14 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *   IKV_E4M3  scale = the least power of two with 448 scale >= a, code_d = x_d / scale
  *             rounded to the nearest E4M3 value, ties to even. A power of two costs a
  *             floating code no precision, and makes reading back exact, in bf16 too. The
- *             attention calls take the scales of E4M3 rows as normal powers of two, or NaN,
- *             whoever wrote them: with any other their results are not defined (the chunk
- *             call uses the power below it). With IKV_DEBUG=1 they refuse one that a token
- *             sees.
+ *             calls take any scale, whoever wrote it; with one that is no normal power of two
+ *             the chunk calls, past the query rows that stay in two parts below, round
+ *             code * scale to bf16 (2^-8) before the products, for float32 outputs too.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
  * every channel. At the top of the range code * scale may round past the largest float and
- * stand for an infinity (E4M3: channels from 248 * 2^120 on). L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer
- * of a larger cache is a descriptor with L = 1 and pointers to that layer.
+ * stand for an infinity (E4M3: channels from 248 * 2^120 on). L, Hq, Hkv, D as for ikv_pool
+ * (D in {64, 128}, Hq / Hkv <= 8). One layer of a larger cache is a descriptor with L = 1 and
+ * pointers to that layer.
  */
 typedef struct ikv_quant_pool {
   int32_t L, Hq, Hkv, D;

@@ -10,7 +10,8 @@
 // waves, two workgroups a CU stage every tile twice as often (3.06 ms against 2.82); of 64 rows a
 // wave the registers spill (6.0 ms).
 //   staging   rows or codes go from HBM through registers, are made bf16 (exactly:
-//             int8 codes as they are, E4M3 ones with their scales, which are powers of two) and
+//             int8 codes as they are, E4M3 ones with their scales where those are powers of two,
+//             as the store writes them; with another scale the product is rounded to bf16) and
 //             written to one of two LDS buffers, the keys a tile before the values: keys
 //             [64][D + 8], values [64][D + 32], strides that spread the reads over all banks
 //   S^T = K Q^T with 32 x 32 x 16 products: lane (h, c) holds entries 8 i + 4 h + (0..3) of
@@ -219,11 +220,13 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         if constexpr (FMT == KV_E4M3) {
           y[0] = e4m3_scaled4(x.x, scale), y[1] = e4m3_scaled4(x.y, scale);
           y[2] = e4m3_scaled4(x.z, scale), y[3] = e4m3_scaled4(x.w, scale);
-          const bool bad = !(fabsf(scale) < INFINITY);
-          if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) y[0] = y[1] = y[2] = y[3] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+          if (__builtin_amdgcn_ballot_w64(no_power(scale)) != 0 && no_power(scale)) {
+            y[0] = e4m3_times4(x.x, scale), y[1] = e4m3_times4(x.y, scale);
+            y[2] = e4m3_times4(x.z, scale), y[3] = e4m3_times4(x.w, scale);
+          }
           // NaN codes, products past the largest bf16 (448 * 2^119 is below it), scales that are not finite
           if (look && __builtin_amdgcn_ballot_w64((e4m3_nans(x.x) | e4m3_nans(x.y) | e4m3_nans(x.z) | e4m3_nans(x.w)) != 0 ||
-                                                  !(fabsf(scale) < 0x1p120f)) != 0) {
+                                                  !(fabsf(scale) < 0x1p119f)) != 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               odd |= odd_low(y[i].x) | odd_high(y[i].x) | odd_low(y[i].y) | odd_high(y[i].y);
@@ -438,17 +441,17 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         } else if constexpr (FMT == KV_E4M3) {
           const Off at = row_at(list[j]);
           const float scale = scale_at(at).y;
-          const bool bad = !(fabsf(scale) < INFINITY);
+          const bool any = no_power(scale);
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
-              const uint2 y = e4m3_scaled4(*reinterpret_cast<const uint32_t *>(vbase + at + (32 * db + 8 * i4 + 4 * h2)), scale);
+              const uint32_t w4 = *reinterpret_cast<const uint32_t *>(vbase + at + (32 * db + 8 * i4 + 4 * h2));
+              const uint2 y = any ? e4m3_times4(w4, scale) : e4m3_scaled4(w4, scale);
               const uint32_t z[4] = {y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float x = bad ? __uint_as_float(0x7fc00000u) : odd_high(z[i]) ? __uint_as_float(z[i]) : 0.f;
-                o[db][4 * i4 + i] += see ? x : 0.f;
+                o[db][4 * i4 + i] += see && odd_high(z[i]) ? __uint_as_float(z[i]) : 0.f;
               }
             }
         } else {

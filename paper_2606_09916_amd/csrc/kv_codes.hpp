@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "attend.hpp"
@@ -26,6 +27,24 @@ template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
 __device__ __forceinline__ uint2 e4m3_scaled4(uint32_t w, float scale) {
   return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
+}
+
+// Whether a scale is anything but a normal power of two: those are 0 .. 253 once the exponent is
+// rotated down, less one; a mantissa, a sign, zero and what is not finite lie above.
+__device__ __forceinline__ bool no_power(float scale) {
+  const uint32_t t = __float_as_uint(scale) - 0x00800000u;
+  return (t >> 23 | t << 9) > 253u;
+}
+
+// The same times any scale, each product rounded to bf16; NaN where the scale is not finite.
+__device__ __forceinline__ uint2 e4m3_times4(uint32_t w, float scale) {
+  if (!(fabsf(scale) < INFINITY)) return make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+  bf16x2_k y[2];
+  y[0][0] = __bf16(__builtin_amdgcn_cvt_f32_fp8(w, 0) * scale);
+  y[0][1] = __bf16(__builtin_amdgcn_cvt_f32_fp8(w, 1) * scale);
+  y[1][0] = __bf16(__builtin_amdgcn_cvt_f32_fp8(w, 2) * scale);
+  y[1][1] = __bf16(__builtin_amdgcn_cvt_f32_fp8(w, 3) * scale);
+  return make_uint2(__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]));
 }
 
 // 4 adjacent codes of a word -> 4 bf16.
