@@ -265,38 +265,6 @@ ikv_status debug_live(const ikv_session *sess, int B, const int32_t *live, const
   return IKV_OK;
 }
 
-// The scales of the E4M3 rows that an attention call's tokens see: normal powers of two, or NaN.
-ikv_status debug_e4m3_scales(const ikv::AttendArgs &a, const ikv_session *sess, int B, bool decode, const int32_t *live,
-                             const int32_t *n_live, int sinks, int window, hipStream_t st) {
-  std::vector<int32_t> h;
-  std::vector<float> sc;
-  for (int b = 0; b < B; ++b) {
-    int64_t nl = 0;
-    if (ikv_status r = debug_count(n_live, b, sess[b].N, st, "n_live", &nl)) return r;
-    const int64_t n = ikv::attend_tokens(sess[b], decode);
-    if (n == 0 || nl == 0) continue;
-    if (ikv_status r = debug_fetch(h, live + sess[b].slot_off, nl, st, "live", b)) return r;
-    const int64_t lo = window ? std::max<int64_t>(0, nl - n - window + 1) : 0, first = std::min<int64_t>(sinks, lo);
-    h.erase(h.begin() + first, h.begin() + lo);    // between the sinks and every window
-    const auto ends = std::minmax_element(h.begin(), h.end());
-    const int64_t least = *ends.first, count = *ends.second - least + 1, pairs = int64_t(a.Hkv) * 2;
-    for (int l = 0; l < a.L; ++l) {
-      const float *from = a.scales + (l * a.num_slots + least) * pairs;
-      if (ikv_status r = debug_fetch(sc, from, count * pairs, st, "scales", b)) return r;
-      for (size_t i = 0; i < h.size(); ++i)
-        for (int64_t k = 0; k < pairs; ++k) {
-          const float x = sc[size_t((h[i] - least) * pairs + k)];
-          int e;
-          if (isnan(x) || (isnormal(x) && frexpf(x, &e) == 0.5f)) continue;
-          const int64_t at = int64_t(i) < first ? int64_t(i) : int64_t(i) + lo - first;
-          return fail(IKV_EINVAL, "IKV_DEBUG: session %d: the %s scale of live[%lld] = slot %d (layer %d, KV head %lld) is %g, not "
-                      "a power of two", b, k % 2 ? "value" : "key", (long long)at, h[i], l, (long long)(k / 2), double(x));
-        }
-    }
-  }
-  return IKV_OK;
-}
-
 // The slot lists of a store into, or a load from, the 8-bit cache, among the entries that are not
 // skipped: ids in range, and no destination listed twice.
 ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache_ids, int64_t cache_slots,
@@ -346,12 +314,7 @@ ikv_status attend(ikv::AttendArgs a, const ikv_session *sess, const ikv_session 
   const ikv::AttendPlan plan = ikv::attend_plan(a, sess, B, decode, sinks, window);
   if (plan.max_n == 0) return ok();
   if (plan.too_large) return fail(IKV_EUNSUPPORTED, "%s: too many sessions, layers, entries or query rows for one launch", what);
-  if (debug_mode()) {
-    if ((r = debug_live(sess, B, live, n_live, a.num_slots, (hipStream_t)stream))) return r;
-    if (a.format == ikv::KV_E4M3 &&
-        (r = debug_e4m3_scales(a, sess, B, decode, live, n_live, window ? sinks : 0, window, (hipStream_t)stream)))
-      return r;
-  }
+  if (debug_mode() && (r = debug_live(sess, B, live, n_live, a.num_slots, (hipStream_t)stream))) return r;
   a.sess = sess_dev, a.B = B, a.decode = decode;
   a.q = q, a.live = live, a.n_live = n_live, a.out = out;
   a.sinks = window ? std::min(sinks, ikv::ATTEND_MOST) : 0, a.window = std::min(window, ikv::ATTEND_MOST);
