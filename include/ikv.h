@@ -443,7 +443,7 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *             rounded to the nearest E4M3 value, ties to even. A power of two costs a
  *             floating code no precision, and makes reading back exact, in bf16 too. The
  *             calls take any scale, whoever wrote it; with one that is no normal power of two
- *             the chunk calls, past the query rows that stay in two parts below, round
+ *             a chunk call of more than 16 query rows a KV head (32 for bf16 outputs) rounds
  *             code * scale to bf16 (2^-8) before the products, for float32 outputs too.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
  * every channel. At the top of the range code * scale may round past the largest float and
@@ -510,9 +510,9 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
  *   out = softmax_j(q . K_j / sqrt(D)) . V_j over the entries seen, logits, softmax statistics
  *     and sums in float32 (of weights up to 2^8 before they are divided). The weights enter the
  *     product with V in bf16 parts: three for float32 outputs (each weight off by 2^-25 of it);
- *     for bf16 outputs two (2^-17) where a KV head has up to 16 query rows (tokens times
- *     Hq / Hkv; 32 over the 8-bit cache), and one (2^-8, to nearest; their sum is of the unrounded
- *     ones) for longer chunks. Entries a token does not see add nothing to it, whatever their
+ *     for bf16 outputs two (2^-17) where the longest chunk of the call has up to 16 query rows a
+ *     KV head (tokens times Hq / Hkv; 32 over the 8-bit cache), and one (2^-8, to nearest; their
+ *     sum is of the unrounded ones) where it has more. Entries a token does not see add nothing to it, whatever their
  *     rows and scales hold.
  *   q, out: device, 16-byte aligned, packed by session (session b's rows start after those of
  *     the sessions before it), [L][Hq][n][D] each: [B][L][Hq][D] for the decode. Their type is
