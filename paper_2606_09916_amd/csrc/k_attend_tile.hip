@@ -25,7 +25,7 @@
 // rounding, and averaged over the entries; their sum is of the unrounded ones): against float64
 // the long chunks are off by 0.0018 to 0.0019 where the output's rounding alone is 0.0017. float32
 // outputs take queries and weights as three bf16 parts, which at D = 128 do not fit the
-// registers: 42 to 67 of a lane's are spilled (8 layers, 200 tokens over 4000: 348 to 377 us). Of the
+// registers: 42 to 67 of a lane's are spilled (8 layers, 200 tokens over 4000: 340 to 377 us). Of the
 // bf16 outputs' instances, int8 with eight waves, and bf16 rows and E4M3 with four, spill two.
 #include <math.h>
 
@@ -204,8 +204,9 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       return !(vb < T && jb <= o0 && (a.window == 0 || jb < a.sinks || ja > o1 - a.window));
     };
     // the values and scales of `tile` (buffer tile & 1) and the keys of tile + 1. A value that is
-    // not finite (a bf16 one, a NaN code, a scale, a product of both) would turn the zero weights of rows that do not see it into NaN: in a tile that
-    // some row does not see whole it is left out and added after the loop.
+    // not finite (a bf16 one, a NaN code, a scale, a product of both) would turn the zero weights
+    // of rows that do not see it into NaN: in a tile that some row does not see whole it is left
+    // out and added after the loop.
     bool odd = false;
     auto put = [&](uint16_t *dst, uint4 x, float scale, bool look) __attribute__((always_inline)) {
       if constexpr (FMT == KV_BF16) {
