@@ -13,8 +13,8 @@ a scale, a power of two, as one byte e for 2^(e - 127), and 32 codes, two a byte
 channel in the lower half. A code is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6. With
 a = max(max|x|, 2^-100) over the block:
   scale  the least power of two s with 7 s >= a, at most 2^125;
-  code   the value nearest x / s, ties to the even code (0, 1, 2, 4 of two neighbours),
-         6 from 5 on.
+  code   the value nearest x / s, ties to the even code (0, 1, 2 or 4 of two neighbours),
+         6 past 5.
 Attention of token t of a session's n newest over its list of live slots (N entries, the n
 newest last), own entry i = N - n + t: entry j is seen if j <= i and, where there is a
 window, j < sinks or j > i - window;
