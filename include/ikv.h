@@ -43,10 +43,10 @@
  *    it). With IKV_DEBUG=1 in the environment (read on every call), the calls
  *    that read such ids (score_history, redirect_slots, decode_attend_slotmap,
  *    compact_apply, prefill_span, quant_store, quant_load, decode_attend_quant,
- *    attend_chunk, attend_chunk_quant) first copy them to the host, after the
- *    stream's earlier work, and return IKV_EINVAL naming the session, the array
- *    and the index of the first bad entry, with no kernel launched. This
- *    synchronises the stream on every call; it is meant for debugging.
+ *    attend_chunk, attend_chunk_quant, return_slots, take_slots) first copy them to
+ *    the host, after the stream's earlier work, and return IKV_EINVAL naming the
+ *    session, the array and the index of the first bad entry, with no kernel
+ *    launched. This synchronises the stream on every call; it is meant for debugging.
  */
 #ifndef IKV_H
 #define IKV_H
@@ -70,9 +70,10 @@ typedef int32_t ikv_status;
 #define IKV_BF16 0
 #define IKV_F32  1
 
-/* Codes of the 8-bit cache (ikv_quant_pool). */
+/* Codes of the quantised cache (ikv_quant_pool): of 8 bits, and of 4. */
 #define IKV_INT8 0
 #define IKV_E4M3 1
+#define IKV_E2M1 4
 
 /* ikv_score_history flags. */
 #define IKV_RESIDUAL  1u   /* add alpha * MLP(phi ++ c), Eq. 4 (needs `residual`)           */
@@ -426,13 +427,16 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
                             void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * The 8-bit cache: K and V rows by physical slot like the pool, each row of one layer,
- * slot and KV head as D one-byte codes and a float32 scale.
+ * The quantised cache: K and V rows by physical slot like the pool, each row of one layer,
+ * slot and KV head as D codes of 8 bits and a float32 scale, or as D codes of 4 bits and a
+ * scale of one byte for each block of 32 channels.
+ *
+ * 8 bits (IKV_INT8, IKV_E4M3):
  *   k_codes, v_codes: device, [L][num_slots][Hkv][D] bytes, 16-byte aligned.
  *   scales: device float32, [L][num_slots][Hkv][2], 8-byte aligned: the scale of the K
  *           row, then of the V row.
  *   code: IKV_INT8 (two's complement, -127 .. 127) or IKV_E4M3 (OCP FP8 E4M3: 4 exponent
- *         and 3 mantissa bits, largest 448).
+ *         and 3 mantissa bits, largest 448); IKV_E2M1: below.
  *   io_dtype: IKV_BF16 or IKV_F32, the type of q and out in the attention calls.
  *   dead_slot: as in ikv_pool; its row is neither written nor read.
  * A row stands for code * scale. With a = max(max_d |x_d|, 2^-100) over the row:
@@ -447,9 +451,25 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *             code * scale to bf16 (2^-8) before the products, for float32 outputs too.
  * A row that holds an infinity or a NaN gets codes 0 and scale NaN: it stands for NaN on
  * every channel. At the top of the range code * scale may round past the largest float and
- * stand for an infinity (E4M3: channels from 248 * 2^120 on). L, Hq, Hkv, D as for ikv_pool
- * (D in {64, 128}, Hq / Hkv <= 8). One layer of a larger cache is a descriptor with L = 1 and
- * pointers to that layer.
+ * stand for an infinity (E4M3: channels from 248 * 2^120 on).
+ *
+ * 4 bits (IKV_E2M1, the OCP MX format MXFP4): a row is D / 32 blocks of 32 adjacent channels.
+ *   k_codes, v_codes: device, [L][num_slots][Hkv][D / 2] bytes, 16-byte aligned; channel 2 i
+ *           in the low four bits of byte i, channel 2 i + 1 in the high ones. A code is a sign
+ *           (bit 3) and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0 to 2).
+ *   scales: device bytes, [L][num_slots][Hkv][2][D / 32], 8-byte aligned: of the K row's
+ *           blocks, then of the V row's. Byte e is the scale 2^(e - 127), 255 is NaN.
+ * With a = max(max_d |x_d|, 2^-100) over the block the store writes
+ *   scale = the least power of two with 7 scale >= a, but at most 2^125 (bytes 25 .. 252);
+ *   code_d = x_d / scale rounded to the nearest value, ties to the even code, 6 past 5.
+ * 7 is 6 and half a step more: channels of scale and above are off by no more than a fifth of
+ * themselves, wherever they lie, smaller ones by no more than scale / 4 (blocks past 7 * 2^125
+ * aside). A block that holds an infinity or a NaN gets codes 0 and the scale NaN: it stands for
+ * NaN on its 32 channels. code * scale is exact in bf16. The calls take any scale byte, whoever
+ * wrote it: with 253 and 254 the largest values stand for infinities.
+ *
+ * L, Hq, Hkv, D as for ikv_pool (D in {64, 128}, Hq / Hkv <= 8). One layer of a larger cache is
+ * a descriptor with L = 1 and pointers to that layer.
  */
 typedef struct ikv_quant_pool {
   int32_t L, Hq, Hkv, D;
@@ -460,11 +480,11 @@ typedef struct ikv_quant_pool {
   int32_t reserved;            /* 0 */
   void *k_codes;
   void *v_codes;
-  float *scales;
+  float *scales;               /* IKV_E2M1: bytes */
 } ikv_quant_pool;
 
 /*
- * Quantise rows of a pool into the 8-bit cache: for session b, k < min(n_rows[b], N) and
+ * Quantise rows of a pool into the quantised cache: for session b, k < min(n_rows[b], N) and
  * every layer and KV head, the K and V rows at slot src[slot_off + k] of `pool` go to slot
  * dst[slot_off + k] of `cache`. Uses: new tokens (a pool of the new rows, src NULL), the
  * kept rows of a retention event (src = dst = the live list), a change of slots.
@@ -483,7 +503,7 @@ ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool,
                            void *stream);
 
 /*
- * Read rows of the 8-bit cache back into a pool: code * scale in float32, rounded to the
+ * Read rows of the quantised cache back into a pool: code * scale in float32, rounded to the
  * pool's type (nearest even), from slot src[slot_off + k] of `cache` to slot
  * dst[slot_off + k] of `pool` (dst NULL: row slot_off + k). Entries whose src is
  * cache->dead_slot are skipped and leave the pool's row as it is. Otherwise as
@@ -495,8 +515,8 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
                           void *stream);
 
 /*
- * Attention over the 8-bit cache, and attention of a chunk of new tokens over a pool or
- * the 8-bit cache.
+ * Attention over the quantised cache, and attention of a chunk of new tokens over a pool or
+ * the quantised cache.
  *   live, n_live: the session's list of slots, oldest first, new tokens last (as
  *     ikv_redirect_slots writes it, the slots of new tokens appended; n_live[b] is clamped
  *     to [0, N]). The new tokens' rows are in the cache already.
@@ -511,7 +531,7 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
  *     and sums in float32 (of weights up to 2^8 before they are divided). The weights enter the
  *     product with V in bf16 parts: three for float32 outputs (each weight off by 2^-25 of it);
  *     for bf16 outputs two (2^-17) where the longest chunk of the call has up to 16 query rows a
- *     KV head (tokens times Hq / Hkv; 32 over the 8-bit cache), and one (2^-8, to nearest; their
+ *     KV head (tokens times Hq / Hkv; 32 over the quantised cache), and one (2^-8, to nearest; their
  *     sum is of the unrounded ones) where it has more. Entries a token does not see add nothing to it, whatever their
  *     rows and scales hold.
  *   q, out: device, 16-byte aligned, packed by session (session b's rows start after those of
@@ -542,9 +562,63 @@ ikv_status ikv_attend_chunk_quant(const ikv_quant_pool *cache, const ikv_session
                                   int32_t window, void *out, void *workspace,
                                   size_t workspace_bytes, void *stream);
 
-/* ikv_workspace_bytes for the calls on the 8-bit cache: IKV_CALL_DECODE or IKV_CALL_CHUNK. */
+/* ikv_workspace_bytes for the calls on the quantised cache: IKV_CALL_DECODE or IKV_CALL_CHUNK. */
 ikv_status ikv_quant_workspace_bytes(const ikv_quant_pool *cache, const ikv_session *sess,
                                      int32_t B, int32_t call, size_t *bytes);
+
+/*
+ * Slots for new tokens. ikv_redirect_slots says which slots a retention event freed; these two
+ * calls keep the free ones as a stack on the device, so that a step returns slots, takes slots
+ * for its new tokens, and lists them, without the host knowing how many.
+ *   num_slots: the pool's slots, and the entries that `slots` has room for.
+ *   dead_slot: as in ikv_pool; it is never free.
+ *   slots: device int32 [num_slots]: entries [0, count[0]) are the free slots, each once.
+ *   count: device int32 [2]: the number of free slots, and a word that the calls use among
+ *          their workgroups: 0 before the first call, and again after each.
+ * Calls on one stack must follow one another (one stream, or events between streams).
+ */
+typedef struct ikv_free_slots {
+  int64_t num_slots;
+  int32_t dead_slot;
+  int32_t reserved;            /* 0 */
+  int32_t *slots;
+  int32_t *count;
+} ikv_free_slots;
+
+/*
+ * Push slots onto the stack: entries list[slot_off + k], k < n_list[b] (clamped to [0, N]), of
+ * session after session, in order. ikv_redirect_slots' freed and n_freed, or live and n_live of
+ * a request that ends. The sentinel and slots that are free already must not be listed; what
+ * would not fit into num_slots entries is dropped. Only N and slot_off of the sessions are read.
+ */
+ikv_status ikv_return_slots(const ikv_free_slots *free_slots, const ikv_session *sess,
+                            const ikv_session *sess_dev, int32_t B, const int32_t *list,
+                            const int32_t *n_list, void *stream);
+
+/*
+ * Take slots for the new tokens of each session: n = qe - qs, its span's, or with n_new (device
+ * int32 [B], for batches whose sessions' tokens the host does not know) n_new[b] clamped to
+ * [0, qe - qs]. Sessions are served whole and in order, as long as the stack holds enough for
+ * all tokens up to theirs: the first session that does not get its tokens, and all after it, get
+ * none. A session whose live list has no room for its tokens (n_live[b] + n > N) gets none
+ * either, and the others do not wait for it. The slots of the T tokens served in all are the
+ * topmost T of the stack, in the stack's order: tokens in order, sessions in order.
+ *   n_taken: device int32 [B]: n, or 0 for a session that got none.
+ * Of a session that is served, token t's slot goes to
+ *   slot_maps[slot_off + qs + t] (NULL: not written): position qs + t;
+ *   live[slot_off + n_live[b] + t]: the end of the live list, n_live[b] clamped to [0, N]. All
+ *     of live, n_live and n_all are NULL, or none;
+ *   dst[slot_off + t] (NULL: not written): the destinations that ikv_quant_store takes for a
+ *     pool of new rows, with n_rows = n_taken.
+ *   n_all: device int32 [B]: the live list's length afterwards, of every session; may be n_live.
+ * Nothing else is written. n_taken may be n_new. Otherwise no two arrays may overlap.
+ * ikv_return_slots with dst and n_taken puts the slots back as they were.
+ * Both calls: at most 2^31 - 1 entries of all sessions together (spans' tokens for the take).
+ */
+ikv_status ikv_take_slots(const ikv_free_slots *free_slots, const ikv_session *sess,
+                          const ikv_session *sess_dev, int32_t B, const int32_t *n_new,
+                          int32_t *slot_maps, int32_t *live, const int32_t *n_live, int32_t *n_all,
+                          int32_t *dst, int32_t *n_taken, void *stream);
 
 /*
  * Workspace size of one call (IKV_CALL_*) for these sessions, in bytes (0 when

@@ -1,4 +1,4 @@
-// Arguments and launch plan of the attention over the 8-bit cache and of the chunk
+// Arguments and launch plan of the attention over the quantised cache and of the chunk
 // attention (k_attend*.hip). Plain C++: no HIP in here.
 #pragma once
 
@@ -12,7 +12,10 @@
 namespace ikv {
 
 // How the rows that attention reads are held.
-enum KvFormat { KV_BF16 = 0, KV_INT8 = 1, KV_E4M3 = 2 };
+enum KvFormat { KV_BF16 = 0, KV_INT8 = 1, KV_E4M3 = 2, KV_E2M1 = 3 };
+
+// Bytes of a row of D channels.
+constexpr int kv_row_bytes(int format, int D) { return format == KV_BF16 ? 2 * D : format == KV_E2M1 ? D / 2 : D; }
 
 struct AttendArgs {
   int L, Hq, Hkv, D;
@@ -20,7 +23,7 @@ struct AttendArgs {
   int format;              // KvFormat
   bool io_f32;             // q and out are float32 (else bf16)
   const void *k, *v;       // rows or codes
-  const float *scales;     // [L][num_slots][Hkv][2] (8-bit formats)
+  const float *scales;     // [L][num_slots][Hkv][2]; KV_E2M1: bytes, [L][num_slots][Hkv][2][D / 32]
   const ikv_session *sess; // device
   int B;
   bool decode;             // one token per session, whatever its span
@@ -32,7 +35,7 @@ struct AttendArgs {
 };
 
 constexpr int FEW_ROWS = 16;        // query rows per KV head up to which one wave holds them all (twice that
-                                    // over the 8-bit cache with bf16 outputs)
+                                    // over the quantised cache with bf16 outputs)
 constexpr int FEW_WAVES = 8;        // of a workgroup of k_attend_few, at most
 constexpr int CUS = 256;            // a round: one workgroup on each
 constexpr int ATTEND_MOST = 1 << 30;       // entries of a list, rows of a KV head, sinks and window

@@ -82,13 +82,23 @@ ikv_status check_quant_pool(const ikv_quant_pool *c) {
   if (c->D != 64 && c->D != 128) return fail(IKV_EUNSUPPORTED, "cache: D = %d (supported: 64, 128)", c->D);
   if (c->num_slots < 1 || c->num_slots > INT32_MAX) return fail(IKV_ESHAPE, "cache: num_slots out of range");
   if (c->dead_slot < 0 || c->dead_slot >= c->num_slots) return fail(IKV_ESHAPE, "cache: dead_slot out of range");
-  if (c->code != IKV_INT8 && c->code != IKV_E4M3) return fail(IKV_EINVAL, "cache: unknown code %d", c->code);
+  if (c->code != IKV_INT8 && c->code != IKV_E4M3 && c->code != IKV_E2M1)
+    return fail(IKV_EINVAL, "cache: unknown code %d", c->code);
   if (c->io_dtype != IKV_BF16 && c->io_dtype != IKV_F32) return fail(IKV_EINVAL, "cache: unknown io_dtype %d", c->io_dtype);
   if (c->reserved != 0) return fail(IKV_EINVAL, "cache: reserved must be 0");
   if (!c->k_codes || !c->v_codes || !c->scales) return fail(IKV_EINVAL, "cache: k_codes / v_codes / scales is NULL");
   if ((reinterpret_cast<uintptr_t>(c->k_codes) | reinterpret_cast<uintptr_t>(c->v_codes)) % 16 ||
       reinterpret_cast<uintptr_t>(c->scales) % 8)
     return fail(IKV_EINVAL, "cache: k_codes and v_codes must be 16-byte aligned, scales 8-byte aligned");
+  return IKV_OK;
+}
+
+ikv_status check_free_slots(const ikv_free_slots *f) {
+  if (!f) return fail(IKV_EINVAL, "free_slots is NULL");
+  if (f->num_slots < 1 || f->num_slots > INT32_MAX) return fail(IKV_ESHAPE, "free_slots: num_slots out of range");
+  if (f->dead_slot < 0 || f->dead_slot >= f->num_slots) return fail(IKV_ESHAPE, "free_slots: dead_slot out of range");
+  if (f->reserved != 0) return fail(IKV_EINVAL, "free_slots: reserved must be 0");
+  if (!f->slots || !f->count) return fail(IKV_EINVAL, "free_slots: slots / count is NULL");
   return IKV_OK;
 }
 
@@ -192,7 +202,7 @@ ikv::AttendArgs attend_args(const ikv_quant_pool *c) {
   ikv::AttendArgs a{};
   a.L = c->L, a.Hq = c->Hq, a.Hkv = c->Hkv, a.D = c->D;
   a.num_slots = c->num_slots;
-  a.format = c->code == IKV_INT8 ? ikv::KV_INT8 : ikv::KV_E4M3;
+  a.format = c->code == IKV_INT8 ? ikv::KV_INT8 : c->code == IKV_E4M3 ? ikv::KV_E4M3 : ikv::KV_E2M1;
   a.io_f32 = c->io_dtype == IKV_F32;
   a.k = c->k_codes, a.v = c->v_codes, a.scales = c->scales;
   return a;
@@ -265,7 +275,7 @@ ikv_status debug_live(const ikv_session *sess, int B, const int32_t *live, const
   return IKV_OK;
 }
 
-// The slot lists of a store into, or a load from, the 8-bit cache, among the entries that are not
+// The slot lists of a store into, or a load from, the quantised cache, among the entries that are not
 // skipped: ids in range, and no destination listed twice.
 ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache_ids, int64_t cache_slots,
                             const char *cache_what, int32_t dead, const int32_t *pool_ids, int64_t pool_slots,
@@ -289,6 +299,25 @@ ikv_status debug_quant_rows(const ikv_session *sess, int B, const int32_t *cache
   std::sort(written.begin(), written.end());
   const auto twice = std::adjacent_find(written.begin(), written.end());
   if (twice != written.end()) return fail(IKV_EINVAL, "IKV_DEBUG: destination slot %d is listed twice", *twice);
+  return IKV_OK;
+}
+
+// A stack of free slots: its count and the calls' word in range, every slot in the pool, not the
+// sentinel and there once. used[slot] says so afterwards.
+ikv_status debug_free_slots(const ikv_free_slots *f, hipStream_t st, int32_t *n_free, std::vector<bool> &used) {
+  std::vector<int32_t> h;
+  if (ikv_status r = debug_fetch(h, f->count, 2, st, "count", 0)) return r;
+  if (h[0] < 0 || h[0] > f->num_slots || h[1] != 0)
+    return fail(IKV_EINVAL, "IKV_DEBUG: free slots: count is (%d, %d), not within [0, %lld] and 0", h[0], h[1], (long long)f->num_slots);
+  *n_free = h[0];
+  if (ikv_status r = debug_fetch(h, f->slots, *n_free, st, "slots", 0)) return r;
+  used.assign(size_t(f->num_slots), false);
+  for (int32_t i = 0; i < *n_free; ++i) {
+    const int32_t u = h[size_t(i)];
+    if (u < 0 || u >= f->num_slots || u == f->dead_slot || used[size_t(u)])
+      return fail(IKV_EINVAL, "IKV_DEBUG: free slots: slots[%d] = %d is outside the pool, the sentinel or there twice", i, u);
+    used[size_t(u)] = true;
+  }
   return IKV_OK;
 }
 
@@ -322,7 +351,7 @@ ikv_status attend(ikv::AttendArgs a, const ikv_session *sess, const ikv_session 
   return hip_status(ikv::launch_attend(a, plan, (hipStream_t)stream), what);
 }
 
-// The checks that the store into and the load from the 8-bit cache share.
+// The checks that the store into and the load from the quantised cache share.
 ikv_status check_quant_rows(const ikv_quant_pool *c, const ikv_pool *p, const ikv_session *sess,
                             const ikv_session *sess_dev, int32_t B, const int32_t *cache_ids, const char *cache_what,
                             const int32_t *pool_ids) {
@@ -815,6 +844,63 @@ ikv_status ikv_attend_chunk_quant(const ikv_quant_pool *cache, const ikv_session
   if (ikv_status r = check_quant_pool(cache)) return r;
   return attend(attend_args(cache), sess, sess_dev, B, false, q, live, n_live, sinks, window, out, workspace,
                 workspace_bytes, stream, "ikv_attend_chunk_quant");
+}
+
+ikv_status ikv_return_slots(const ikv_free_slots *free_slots, const ikv_session *sess, const ikv_session *sess_dev,
+                            int32_t B, const int32_t *list, const int32_t *n_list, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  ikv_status r = check_free_slots(free_slots);
+  if (r) return r;
+  if ((r = check_sessions(sess, sess_dev, B))) return r;
+  if (B == 0) return ok();
+  if (!list || !n_list) return fail(IKV_EINVAL, "list / n_list is NULL");
+  int64_t entries = 0;
+  for (int b = 0; b < B; ++b) entries += sess[b].N;
+  if (entries > INT32_MAX) return fail(IKV_EUNSUPPORTED, "ikv_return_slots: more than 2^31 - 1 entries");
+  if (debug_mode()) {
+    const hipStream_t st = (hipStream_t)stream;
+    std::vector<bool> used;
+    std::vector<int32_t> h;
+    int32_t n_free = 0;
+    if ((r = debug_free_slots(free_slots, st, &n_free, used))) return r;
+    for (int b = 0; b < B; ++b) {
+      int64_t n = 0;
+      if ((r = debug_count(n_list, b, sess[b].N, st, "n_list", &n))) return r;
+      if ((r = debug_fetch(h, list + sess[b].slot_off, n, st, "list", b))) return r;
+      for (int64_t k = 0; k < n; ++k) {
+        const int32_t u = h[size_t(k)];
+        if ((r = debug_id(u, k, 0, free_slots->num_slots, "list", b))) return r;
+        if (u == free_slots->dead_slot || used[size_t(u)])
+          return fail(IKV_EINVAL, "IKV_DEBUG: session %d: list[%lld] = %d is the sentinel or free already", b, (long long)k, u);
+        used[size_t(u)] = true;
+      }
+    }
+  }
+  return hip_status(ikv::launch_return_slots(*free_slots, sess_dev, B, entries, list, n_list, (hipStream_t)stream),
+                    "ikv_return_slots");
+}
+
+ikv_status ikv_take_slots(const ikv_free_slots *free_slots, const ikv_session *sess, const ikv_session *sess_dev,
+                          int32_t B, const int32_t *n_new, int32_t *slot_maps, int32_t *live, const int32_t *n_live,
+                          int32_t *n_all, int32_t *dst, int32_t *n_taken, void *stream) {
+  if (ikv_status f = pending_fault()) return f;
+  ikv_status r = check_free_slots(free_slots);
+  if (r) return r;
+  if ((r = check_sessions(sess, sess_dev, B))) return r;
+  if (B == 0) return ok();
+  if (!n_taken) return fail(IKV_EINVAL, "n_taken is NULL");
+  if (!live != !n_live || !live != !n_all) return fail(IKV_EINVAL, "live, n_live and n_all must be given together");
+  int64_t tokens = 0;
+  for (int b = 0; b < B; ++b) tokens += sess[b].qe - sess[b].qs;
+  if (tokens > INT32_MAX) return fail(IKV_EUNSUPPORTED, "ikv_take_slots: more than 2^31 - 1 tokens");
+  if (debug_mode()) {
+    std::vector<bool> used;
+    int32_t n_free = 0;
+    if ((r = debug_free_slots(free_slots, (hipStream_t)stream, &n_free, used))) return r;
+  }
+  return hip_status(ikv::launch_take_slots(*free_slots, sess_dev, B, tokens, n_new, slot_maps, live, n_live, n_all, dst,
+                                           n_taken, (hipStream_t)stream),
+                    "ikv_take_slots");
 }
 
 }  // extern "C"

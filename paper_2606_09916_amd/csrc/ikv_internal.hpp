@@ -332,6 +332,12 @@ hipError_t launch_attend_tile(const AttendArgs &a, const AttendPlan &p, hipStrea
 hipError_t launch_attend_merge(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 
+hipError_t launch_return_slots(const ikv_free_slots &f, const ikv_session *sess_dev, int B, int64_t entries,
+                               const int32_t *list, const int32_t *n_list, hipStream_t st);
+hipError_t launch_take_slots(const ikv_free_slots &f, const ikv_session *sess_dev, int B, int64_t tokens,
+                             const int32_t *n_new, int32_t *slot_maps, int32_t *live, const int32_t *n_live,
+                             int32_t *n_all, int32_t *dst, int32_t *n_taken, hipStream_t st);
+
 // A word of pinned host memory that kernels set (system scope) to report a fault the
 // host cannot see otherwise (a grid barrier that gave up). Allocated on first use and
 // kept for the life of the process; nullptr if the allocation failed. take_host_fault()

@@ -1,6 +1,6 @@
 // Attention of few query rows: the decode of one token, or a chunk of a few tokens whose
 // rows (n tokens x Hq / Hkv heads) of a KV head fit one 16-row matrix block, or two (NR) over
-// the 8-bit cache with bf16 outputs (the other types' registers hold one).
+// the quantised cache with bf16 outputs (the other types' registers hold one).
 //
 // Bound by reading the rows of the list once (2 D + 8 bytes per entry, head and layer in
 // 8-bit form, 4 D in bf16): 36 layers x 8 heads x 8192 int8 entries in 105 us (5.9 TB/s), bf16
@@ -54,15 +54,16 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_k (&o)[P
 template <int FMT, typename IO, int D, int NR, bool O32>
 __global__ void __launch_bounds__(64 * FEW_WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 k_attend_few(AttendArgs a, int heads, int rows_max) {
-  constexpr int ES = FMT == KV_BF16 ? 2 : 1;     // bytes per element
+  constexpr bool SCALED = FMT == KV_INT8 || FMT == KV_E4M3;        // a float32 scale per row
+  constexpr int RB = kv_row_bytes(FMT, D);
   constexpr int KS = D / 32;                     // 32-channel steps of the first product
   constexpr int NC = D / 16;                     // channels of a lane in the second
-  constexpr int KW = D * ES / 64;                // 16-byte loads of a lane per 16 key rows
-  constexpr int VW = NC * ES / 4;                // words of a lane per value row
+  constexpr int KW = RB / 64;                    // 16-byte loads of a lane per 16 key rows (none: one of 8)
+  constexpr int VW = (RB + 63) / 64;             // words of a lane per value row
   constexpr int QP = sizeof(IO) == 4 ? 3 : 1;    // bf16 parts of the queries
   constexpr int PP = sizeof(IO) == 4 ? 3 : 2;    // and of the weights
   constexpr int NB = 2;                          // blocks of entries in registers (three or four: no faster)
-  __shared__ __align__(16) float sc[FEW_WAVES][2][FEW_BLOCK];
+  __shared__ __align__(16) float sc[FEW_WAVES][2][FEW_BLOCK];     // E2M1: key scale words; value scale bytes by block
   extern __shared__ float joint[];               // the parts' states, where a head has several waves
 
   const int b = blockIdx.z;
@@ -115,28 +116,30 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
     for (int k = 0; k < NR; ++k)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int ch = FMT == KV_BF16 ? 32 * ks + 8 * g : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
+        const int ch = FMT == KV_BF16   ? 32 * ks + 8 * g
+                       : FMT == KV_E2M1 ? D / 4 * g + 8 * ks
+                                        : 64 * (ks >> 1) + 16 * g + 8 * (ks & 1);
         float x[8];
         load8(static_cast<const IO *>(a.q) + q_at[k] + ch, x);
         split_parts<QP>(x, qf[k][ks]);
       }
-    const uint32_t row_bytes = uint32_t(a.Hkv) * D * ES;
+    const uint32_t row_bytes = uint32_t(a.Hkv) * RB;
     const int64_t layer = int64_t(l) * a.num_slots;
     // wave-uniform bases; a row is a per-lane byte offset, 32 bits wide where a layer is below 4 GB
-    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES;
-    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES;
+    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * RB;
+    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * RB;
     auto row_at = [&](int sl, uint32_t within) {
       if constexpr (O32) return uint32_t(sl) * row_bytes + within;
       else return uint64_t(uint32_t(sl)) * row_bytes + within;
     };
-    const float2 *sbase = reinterpret_cast<const float2 *>(a.scales) + layer * a.Hkv + hkv;
+    const char *sbase = reinterpret_cast<const char *>(a.scales) + (layer * a.Hkv + hkv) * (SCALED ? 8 : D / 16);
     const int32_t *list = a.live + s.slot_off;
     const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
 
     struct Block {
-      uint4 k[2][KW];
+      uint4 k[2][KW ? KW : 1];
       uint32_t v[8][VW];
-      float2 s;
+      float2 s;                                    // E2M1: the bytes of the key's blocks, of the value's
     };
     // slot of index base + (lane & 31), the last index's past the end
     auto slots = [&](int base) __attribute__((always_inline)) {
@@ -146,19 +149,25 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
     // Value rows go past the caches (nothing reads them again: 123 -> 113 us at 8192 entries); key
     // rows do not, since two loads of 64 bytes share each of their lines (so: 121).
     auto load = [&](Block &x, int sl) __attribute__((always_inline)) {
-      if constexpr (FMT != KV_BF16)                // in the order of use
-        x.s = *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(sbase) + row_at(sl, 0) / (D / 8));
+      if constexpr (SCALED) x.s = *reinterpret_cast<const float2 *>(sbase + row_at(sl, 0) / (D / 8));     // in the order of use
+      else if constexpr (FMT == KV_E2M1 && D == 128) x.s = *reinterpret_cast<const float2 *>(sbase + row_at(sl, 0) / 8);
+      else if constexpr (FMT == KV_E2M1) x.s.x = *reinterpret_cast<const float *>(sbase + row_at(sl, 0) / 8);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const char *p = kbase + row_at(__builtin_amdgcn_ds_bpermute(4 * (16 * kb + c), sl), 16 * g);
+        const char *p = kbase + row_at(__builtin_amdgcn_ds_bpermute(4 * (16 * kb + c), sl), (KW ? 16 : 8) * g);
 #pragma unroll
         for (int j = 0; j < KW; ++j) x.k[kb][j] = *reinterpret_cast<const uint4 *>(p + 64 * j);
+        if constexpr (KW == 0) {
+          const uint2 y = *reinterpret_cast<const uint2 *>(p);
+          x.k[kb][0].x = y.x, x.k[kb][0].y = y.y;
+        }
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int at = e < 4 ? 4 * g + e : 16 + 4 * g + e - 4;
-        const char *p = vbase + row_at(__builtin_amdgcn_ds_bpermute(4 * at, sl), c * (NC * ES));
-        if constexpr (VW == 1) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
+        const char *p = vbase + row_at(__builtin_amdgcn_ds_bpermute(4 * at, sl), c * (RB / 16));
+        if constexpr (RB == 32) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t *>(p));
+        else if constexpr (VW == 1) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
         else if constexpr (VW == 2) {
           const u32x2_few y = __builtin_nontemporal_load(reinterpret_cast<const u32x2_few *>(p));
           x.v[e][0] = y.x;
@@ -177,11 +186,30 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       f32x4_k acc[NR][2];
 #pragma unroll
       for (int k = 0; k < NR; ++k) acc[k][0] = acc[k][1] = f32x4_k{0.f, 0.f, 0.f, 0.f};
-      if constexpr (FMT != KV_BF16) {
+      if constexpr (SCALED) {
         if (lane < FEW_BLOCK) {
           sc[w][0][lane] = x.s.x * to_log2;
           sc[w][1][lane] = x.s.y;
         }
+      }
+      float kscale[2];                             // E2M1: of this lane's block of key row 16 kb + c
+      uint32_t vscale[2];                          // and the bytes of its values' blocks, in the order of x.v
+      if constexpr (FMT == KV_E2M1) {
+        uint8_t *vb = reinterpret_cast<uint8_t *>(sc[w][1]);
+        if (lane < FEW_BLOCK) {
+          const uint32_t kw = __float_as_uint(x.s.x), vw = D == 128 ? __float_as_uint(x.s.y) : kw >> 16;
+          sc[w][0][lane] = __uint_as_float(kw);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) vb[FEW_BLOCK * i + lane] = uint8_t(vw >> (8 * i));
+        }
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          kscale[kb] = __uint_as_float(uint32_t(reinterpret_cast<uint8_t *>(&sc[w][0][16 * kb + c])[D == 128 ? g : g >> 1]) << 23);
+          vscale[kb] = *reinterpret_cast<uint32_t *>(vb + FEW_BLOCK * (c * NC / 32) + 16 * kb + 4 * g);
+        }
+        __builtin_amdgcn_wave_barrier();
       }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -189,6 +217,7 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         for (int ks = 0; ks < KS; ++ks) {
           uint4 u;
           if constexpr (FMT == KV_BF16) u = x.k[kb][ks];
+          else if constexpr (FMT == KV_E2M1) u = e2m1_scaled8((&x.k[kb][0].x)[ks], kscale[kb]);
           else {
             const uint4 y = x.k[kb][ks >> 1];
             const uint2 p = codes4<FMT>(ks & 1 ? y.z : y.x), q = codes4<FMT>(ks & 1 ? y.w : y.y);
@@ -202,7 +231,7 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
               acc[k][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[k][ks][p], acc[k][kb], 0, 0, 0);
         }
       float4 vs[2];
-      if constexpr (FMT != KV_BF16) {
+      if constexpr (SCALED) {
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -260,7 +289,7 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
           for (int i = 0; i < 4; ++i) {
             float p = __builtin_amdgcn_exp2f(acc[k][kb][i] - ms);
             lsum[k] += p;
-            if constexpr (FMT != KV_BF16) {
+            if constexpr (SCALED) {
               p *= (&vs[kb].x)[i];
               if (hidden >> (4 * kb + i) & 1) p = 0.f;      // the scale of an unseen row may be anything
             }
@@ -268,7 +297,17 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
           }
         split_parts<PP>(pw, pf[k]);
       }
-      if constexpr (FMT != KV_INT8) {
+      if constexpr (FMT == KV_E2M1) {
+        if (!whole && __builtin_amdgcn_ballot_w64(scales_odd(vscale[0]) | scales_odd(vscale[1])) != 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t byte = vscale[e >> 2] >> (8 * (e & 3)) & 255u, z = e2m1_odd(x.v[e][0], byte);
+            odd |= z != 0;
+            x.v[e][0] &= ~z;
+            if (byte == 255u) vscale[e >> 2] &= ~(255u << (8 * (e & 3)));
+          }
+        }
+      } else if constexpr (FMT != KV_INT8) {
         if (!whole) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -286,13 +325,21 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         }
       }
       // the operand of channels NC c + STEP k .. at a time
-      constexpr int STEP = FMT == KV_BF16 ? 2 : 4;
+      constexpr int STEP = FMT == KV_BF16 ? 2 : FMT == KV_E2M1 ? NC : 4;
 #pragma unroll
       for (int k = 0; k < VW; ++k) {
         uint32_t f[STEP][4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          if constexpr (FMT == KV_BF16) {
+          if constexpr (FMT == KV_E2M1) {
+            const uint4 y0 = e2m1_scaled8(x.v[2 * p][0], scale_byte(vscale[p >> 1], 2 * p & 3));
+            const uint4 y1 = e2m1_scaled8(x.v[2 * p + 1][0], scale_byte(vscale[p >> 1], (2 * p & 3) + 1));
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) {
+              f[2 * i][p] = __builtin_amdgcn_perm((&y1.x)[i], (&y0.x)[i], 0x05040100u);
+              f[2 * i + 1][p] = __builtin_amdgcn_perm((&y1.x)[i], (&y0.x)[i], 0x07060302u);
+            }
+          } else if constexpr (FMT == KV_BF16) {
             f[0][p] = __builtin_amdgcn_perm(x.v[2 * p + 1][k], x.v[2 * p][k], 0x05040100u);
             f[1][p] = __builtin_amdgcn_perm(x.v[2 * p + 1][k], x.v[2 * p][k], 0x07060302u);
           } else {
@@ -351,6 +398,11 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
                 if constexpr (FMT == KV_BF16) {
                   const uint16_t y = reinterpret_cast<const uint16_t *>(row)[ch];
                   o[k][j][i] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
+                } else if constexpr (FMT == KV_E2M1) {
+                  const uint32_t byte = reinterpret_cast<const uint8_t *>(sbase + row_at(list[e], 0) / 8)[D / 32 + ch / 32];
+                  const uint32_t w = uint32_t(reinterpret_cast<const uint8_t *>(row)[ch / 2]) >> (4 * (ch & 1)) & 15u;
+                  if (see && e2m1_odd(w, byte) != 0)
+                    o[k][j][i] += byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x7f800000u | w >> 3 << 31);
                 } else {
                   o[k][j][i] += see && (row[ch] & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
                 }
@@ -428,7 +480,7 @@ static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   KTimer kt_("k_attend_few", st);
   const dim3 grid(unsigned(p.splits), unsigned(a.L * (a.Hkv / p.heads)), unsigned(a.B));
   const size_t lds = size_t(p.parts - 1) * p.heads * NR * (D / 4 + 2) * WAVE * sizeof(float);
-  if (a.num_slots * a.Hkv * D * (FMT == KV_BF16 ? 2 : 1) < (int64_t(1) << 32))
+  if (a.num_slots * a.Hkv * kv_row_bytes(FMT, D) < (int64_t(1) << 32))
     k_attend_few<FMT, IO, D, NR, true><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
   else
     k_attend_few<FMT, IO, D, NR, false><<<grid, WAVE * p.heads * p.parts, lds, st>>>(a, p.heads, p.rows);
@@ -445,7 +497,8 @@ static void go_few_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
 hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   if (a.format == KV_BF16) go_few_d<KV_BF16, uint16_t>(a, p, st);
   else if (a.format == KV_INT8) a.io_f32 ? go_few_d<KV_INT8, float>(a, p, st) : go_few_d<KV_INT8, uint16_t>(a, p, st);
-  else a.io_f32 ? go_few_d<KV_E4M3, float>(a, p, st) : go_few_d<KV_E4M3, uint16_t>(a, p, st);
+  else if (a.format == KV_E4M3) a.io_f32 ? go_few_d<KV_E4M3, float>(a, p, st) : go_few_d<KV_E4M3, uint16_t>(a, p, st);
+  else a.io_f32 ? go_few_d<KV_E2M1, float>(a, p, st) : go_few_d<KV_E2M1, uint16_t>(a, p, st);
   return p.splits > 1 ? launch_attend_merge(a, p, st) : hipGetLastError();
 }
 

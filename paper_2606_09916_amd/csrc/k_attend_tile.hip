@@ -64,11 +64,12 @@ __device__ __forceinline__ void tile_parts(const float *x, bf16x8_k (&o)[PARTS])
 template <int FMT, typename IO, int D, int NW, bool O32>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
-  constexpr int ES = FMT == KV_BF16 ? 2 : 1;
+  constexpr int RB = kv_row_bytes(FMT, D);
   constexpr int NT = 64 * NW, ROWS = 32 * NW;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int KROW = D + 8, VROW = D + 32;
-  constexpr int PPR = D * ES / 16;               // 16-byte pieces of a row
+  constexpr int PB = RB < 64 ? 8 : 16;           // bytes of a piece
+  constexpr int PPR = RB / PB;                   // pieces of a row
   constexpr int PIECES = TILE_KEYS * PPR;        // of a tile's keys (as many of its values)
   constexpr int PP_ = PIECES > NT ? PIECES / NT : 1;       // pieces of keys, and of values, of a thread
   constexpr int QP = sizeof(IO) == 4 ? 3 : 1, PP = QP;
@@ -125,16 +126,16 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       load8(static_cast<const IO *>(a.q) + q_at + 16 * ks + 8 * h2, x);
       tile_parts<QP>(x, qf[ks]);
     }
-    const uint32_t row_bytes = uint32_t(a.Hkv) * D * ES;
+    const uint32_t row_bytes = uint32_t(a.Hkv) * RB;
     // byte offset of a slot's row: 32 bits, by a 24-bit product, where slots, rows and layers are small enough
     auto row_at = [&](int sl) __attribute__((always_inline)) {
       if constexpr (O32) return uint32_t(__umul24(uint32_t(sl), row_bytes));
       else return uint64_t(uint32_t(sl)) * row_bytes;
     };
     const int64_t layer = int64_t(l) * a.num_slots;
-    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * D * ES;
-    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * D * ES;
-    const float2 *sbase = reinterpret_cast<const float2 *>(a.scales) + layer * a.Hkv + hkv;
+    const char *kbase = static_cast<const char *>(a.k) + (layer * a.Hkv + hkv) * RB;
+    const char *vbase = static_cast<const char *>(a.v) + (layer * a.Hkv + hkv) * RB;
+    const char *sbase = reinterpret_cast<const char *>(a.scales) + (layer * a.Hkv + hkv) * (FMT == KV_E2M1 ? D / 16 : 8);
     const int32_t *list = a.live + s.slot_off;
     const float to_log2 = 1.4426950408889634f / sqrtf(float(D));
 
@@ -148,7 +149,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     struct Regs {
       uint4 k[PP_], v[PP_];
       float2 sc;                                   // int8: of entry `lane`
-      float ks[PP_], vs[PP_];                      // E4M3: of the pieces' rows
+      float ks[PP_], vs[PP_];                      // E4M3: of the pieces' rows; E2M1: of their blocks
     };
     struct Slots { int32_t s[PP_], sc; };
     struct Offs { Off o[PP_], sc; };
@@ -175,24 +176,36 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     auto offsets = [&](const Slots &x) __attribute__((always_inline)) {
       Offs y;
 #pragma unroll
-      for (int i = 0; i < PP_; ++i) y.o[i] = row_at(x.s[i]) + Off(tid % PPR * 16);
+      for (int i = 0; i < PP_; ++i) y.o[i] = row_at(x.s[i]) + Off(tid % PPR * PB);
       if constexpr (FMT == KV_INT8) y.sc = row_at(x.sc);
       return y;
     };
     auto scale_at = [&](Off row) __attribute__((always_inline)) {           // of a row offset: 8 bytes for D
-      return *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(sbase) + (row / D) * 8);
+      return *reinterpret_cast<const float2 *>(sbase + (row / D) * 8);
+    };
+    // E2M1: of the block that holds a piece, by its byte offset; i: of keys (0), of values (1)
+    auto block_scale = [&](Off piece, int i) __attribute__((always_inline)) {
+      const uint8_t *p = reinterpret_cast<const uint8_t *>(sbase) + piece / RB * (D / 16) + piece % RB / 16;
+      return __uint_as_float(uint32_t(p[i * (D / 32)]) << 23);
+    };
+    auto piece_at = [](const char *p) __attribute__((always_inline)) {
+      if constexpr (PB == 16) return *reinterpret_cast<const uint4 *>(p);
+      const uint2 x = *reinterpret_cast<const uint2 *>(p);
+      return make_uint4(x.x, x.y, 0u, 0u);
     };
     // the keys of one tile (offsets k) and the values and scales of the one before (offsets v)
     auto load = [&](const Offs &k, const Offs &v, Regs &r) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PP_; ++i) {
         if (takes_k) {
-          r.k[i] = *reinterpret_cast<const uint4 *>(kbase + k.o[i]);
+          r.k[i] = piece_at(kbase + k.o[i]);
           if constexpr (FMT == KV_E4M3) r.ks[i] = scale_at(k.o[i]).x;
+          if constexpr (FMT == KV_E2M1) r.ks[i] = block_scale(k.o[i], 0);
         }
         if (takes_v) {
-          r.v[i] = *reinterpret_cast<const uint4 *>(vbase + v.o[i]);
+          r.v[i] = piece_at(vbase + v.o[i]);
           if constexpr (FMT == KV_E4M3) r.vs[i] = scale_at(v.o[i]).y;
+          if constexpr (FMT == KV_E2M1) r.vs[i] = block_scale(v.o[i], 1);
         }
       }
       if constexpr (FMT == KV_INT8) r.sc = scale_at(v.sc);
@@ -216,6 +229,18 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
           x = make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w));
         }
         *reinterpret_cast<uint4 *>(dst) = x;
+      } else if constexpr (FMT == KV_E2M1) {
+        if (look && __builtin_amdgcn_ballot_w64(!(fabsf(scale) < 0x1p126f)) != 0) {
+#pragma unroll
+          for (int i = 0; i < PB / 4; ++i) {
+            const uint32_t z = e2m1_odd((&x.x)[i], __float_as_uint(scale) >> 23);
+            odd |= z != 0;
+            (&x.x)[i] &= ~z;
+          }
+          if (!(fabsf(scale) < INFINITY)) scale = 1.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < PB / 4; ++i) reinterpret_cast<uint4 *>(dst)[i] = e2m1_scaled8((&x.x)[i], scale);
       } else {
         uint2 y[4];
         if constexpr (FMT == KV_E4M3) {
@@ -243,7 +268,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     };
     auto store = [&](const Regs &r, int tile, int par) __attribute__((always_inline)) {
       const bool look = edge(tile, own0, own1);
-      constexpr int EL = 16 / ES;                  // elements of a piece
+      constexpr int EL = D / PPR;                  // elements of a piece
       const int at = tid % PPR * EL;
 #pragma unroll
       for (int i = 0; i < PP_; ++i) {
@@ -426,7 +451,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     }
     // (the hint keeps E4M3's out of the loop's registers: 8 float32 layers, 20 tokens over 4000: 83 us, 87 without)
     const bool again = __syncthreads_or(odd);
-    if (FMT == KV_E4M3 ? __builtin_expect(again, false) : again)
+    if (FMT == KV_E4M3 || FMT == KV_E2M1 ? __builtin_expect(again, false) : again)
       for (int v = tb * TILE_KEYS; v < min(T, te * TILE_KEYS); ++v) {
         const int j = v < first ? v : v + gap;
         const bool see = (j <= own) & ((a.window == 0) | (j < a.sinks) | (j > own - a.window));
@@ -439,6 +464,19 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
               const uint16_t y = vrow[32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3)];
               o[db][k] += see && odd_low(y) ? Store<uint16_t>::ld(&y) : 0.f;
             }
+        } else if constexpr (FMT == KV_E2M1) {
+          const Off at = row_at(list[j]);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const uint32_t byte = __float_as_uint(block_scale(at + 16 * db, 1)) >> 23;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const int ch = 32 * db + 8 * (k >> 2) + 4 * h2 + (k & 3);
+              const uint32_t w4 = uint32_t(reinterpret_cast<const uint8_t *>(vbase + at)[ch / 2]) >> (4 * (ch & 1)) & 15u;
+              if (see && e2m1_odd(w4, byte) != 0)
+                o[db][k] += byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x7f800000u | w4 >> 3 << 31);
+            }
+          }
         } else if constexpr (FMT == KV_E4M3) {
           const Off at = row_at(list[j]);
           const float scale = scale_at(at).y;
@@ -501,7 +539,7 @@ static void go_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   const int units = a.B * a.L * a.Hkv;
   KTimer kt_("k_attend_tile", st);
   const dim3 grid(unsigned((units + 7) / 8 * 8 * p.blocks * p.splits));
-  const int64_t row = int64_t(a.Hkv) * D * (FMT == KV_BF16 ? 2 : 1);
+  const int64_t row = int64_t(a.Hkv) * kv_row_bytes(FMT, D);
   if (a.num_slots <= (1 << 24) && row < (1 << 24) && a.num_slots * row <= (int64_t(1) << 32))
     k_attend_tile<FMT, IO, D, NW, true><<<grid, 64 * NW, 0, st>>>(a, p.blocks, p.splits, units);
   else
@@ -518,7 +556,8 @@ static hipError_t go_tile_d(const AttendArgs &a, const AttendPlan &p, hipStream_
 hipError_t launch_attend_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   if (a.format == KV_BF16) return go_tile_d<KV_BF16, uint16_t>(a, p, st);
   if (a.format == KV_INT8) return a.io_f32 ? go_tile_d<KV_INT8, float>(a, p, st) : go_tile_d<KV_INT8, uint16_t>(a, p, st);
-  return a.io_f32 ? go_tile_d<KV_E4M3, float>(a, p, st) : go_tile_d<KV_E4M3, uint16_t>(a, p, st);
+  if (a.format == KV_E4M3) return a.io_f32 ? go_tile_d<KV_E4M3, float>(a, p, st) : go_tile_d<KV_E4M3, uint16_t>(a, p, st);
+  return a.io_f32 ? go_tile_d<KV_E2M1, float>(a, p, st) : go_tile_d<KV_E2M1, uint16_t>(a, p, st);
 }
 
 }  // namespace ikv

@@ -1,4 +1,4 @@
-// Rows between a pool (bf16 or float32) and the 8-bit cache, by slot lists.
+// Rows between a pool (bf16 or float32) and the quantised cache, by slot lists.
 //
 // A row (one layer, slot and KV head; K or V) of D channels belongs to D / 8 adjacent
 // lanes, 8 channels each.
@@ -13,7 +13,10 @@
 //         (ties missed by no less than 2^-33).
 //   e4m3  scale = 2^e with 448 2^e >= a > 224 2^e: x / scale is exact, and the conversion
 //         rounds once.
+//   e2m1  the same over the 32 channels of 4 lanes, with 7 2^e >= a > 7 2^(e - 1), e <= 125: the
+//         conversion divides by 2^e, rounds once and holds what passes 6 there.
 #include "ikv_internal.hpp"
+#include "kv_codes.hpp"
 #include "quant_rows.hpp"
 
 namespace ikv {
@@ -86,6 +89,24 @@ __device__ __forceinline__ uint2 quant8(const float (&x)[8], uint32_t amax_bits,
   return make_uint2(w[0], w[1]);
 }
 
+// The same in 4 bits: 8 codes of a word; amax that of the block, *byte its scale.
+__device__ __forceinline__ uint32_t quant8_e2m1(const float (&x)[8], uint32_t amax_bits, uint8_t *byte) {
+  if (amax_bits >= 0x7f800000u) {
+    *byte = 255;
+    return 0u;
+  }
+  // a = m 2^E, 1 <= m < 2, and 7 = 1.75 * 2^2: e = E - 2, one more where m > 1.75
+  const uint32_t b = __float_as_uint(fmaxf(__uint_as_float(amax_bits), 0x1p-100f));
+  const int e = min(int(b >> 23) - 127 - 2 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), 125);
+  const float scale = __uint_as_float(uint32_t(e + 127) << 23);
+  *byte = uint8_t(e + 127);
+  uint32_t w = 0u;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+}
+
 __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n_rows, int b) {
   return n_rows ? max(0, min(n_rows[b], s.N)) : s.N;
 }
@@ -97,10 +118,10 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
 // 350 us (5.2 TB/s read and written), read back in 311 (5.9); with one place a thread both took
 // 1331, with eight 666.
 
-template <typename T, int D>
+template <typename T, int D, bool FOUR>
 __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool, const T *__restrict__ vpool,
                                                     int64_t pool_slots, uint8_t *__restrict__ kc,
-                                                    uint8_t *__restrict__ vc, float *__restrict__ scales,
+                                                    uint8_t *__restrict__ vc, void *__restrict__ scales,
                                                     int64_t num_slots, int Hkv, int code, int dead, int group,
                                                     const ikv_session *__restrict__ sess,
                                                     const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
@@ -136,6 +157,7 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
       if (at[u] < 0) continue;                     // the lanes of a row go together
       uint2 w[2];
       float sc[2];
+      uint8_t byte[2];
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         float x[8];
@@ -144,15 +166,39 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
 #pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
-        w[kv] = quant8<T>(x, m, code, &sc[kv]);
+        for (int o = 1; o < (FOUR ? 4 : LPR); o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
+        if constexpr (FOUR) w[kv].x = quant8_e2m1(x, m, &byte[kv]);
+        else w[kv] = quant8<T>(x, m, code, &sc[kv]);
       }
       const int64_t row = to[u] + at[u] / LPR;
       const int piece = at[u] % LPR;
+      if constexpr (FOUR) {
+        *reinterpret_cast<uint32_t *>(kc + row * (D / 2) + piece * 4) = w[0].x;
+        *reinterpret_cast<uint32_t *>(vc + row * (D / 2) + piece * 4) = w[1].x;
+        if (piece % 4 == 0) {
+          uint8_t *p = static_cast<uint8_t *>(scales) + row * (D / 16) + piece / 4;
+          p[0] = byte[0];
+          p[D / 32] = byte[1];
+        }
+        continue;
+      }
       *reinterpret_cast<uint2 *>(kc + row * D + piece * 8) = w[0];
       *reinterpret_cast<uint2 *>(vc + row * D + piece * 8) = w[1];
       if (piece == 0) reinterpret_cast<float2 *>(scales)[row] = make_float2(sc[0], sc[1]);
     }
+  }
+}
+
+// 8 codes of a word times their block's scale, exactly, to the pool's type.
+template <typename T> __device__ __forceinline__ void put8_e2m1(T *o, uint32_t w, uint8_t byte) {
+  const float scale = __uint_as_float(uint32_t(byte) << 23);           // 255: NaN
+  if constexpr (sizeof(T) == 4) {
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+    const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+    reinterpret_cast<float4 *>(o)[0] = make_float4(a[0], a[1], b[0], b[1]);
+    reinterpret_cast<float4 *>(o)[1] = make_float4(c[0], c[1], d[0], d[1]);
+  } else {
+    *reinterpret_cast<uint4 *>(o) = e2m1_scaled8(w, scale);
   }
 }
 
@@ -177,9 +223,9 @@ template <typename T> __device__ __forceinline__ void put8(T *o, uint2 w, float 
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool FOUR>
 __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
-                                                   const float *__restrict__ scales, int64_t num_slots, int Hkv,
+                                                   const void *__restrict__ scales, int64_t num_slots, int Hkv,
                                                    int code, int dead, int group, T *__restrict__ kpool,
                                                    T *__restrict__ vpool, int64_t pool_slots,
                                                    const ikv_session *__restrict__ sess,
@@ -194,6 +240,7 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
   for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
     uint2 wk[QU], wv[QU];
     float2 sc[QU];
+    uint8_t bk[QU], bv[QU];
     int64_t to[QU], from[QU];
     bool on[QU];
 #pragma unroll
@@ -208,13 +255,24 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
 #pragma unroll
     for (int u = 0; u < QU; ++u)
       if (on[u]) {
-        wk[u] = reinterpret_cast<const uint2 *>(kc)[from[u]];
-        wv[u] = reinterpret_cast<const uint2 *>(vc)[from[u]];
-        sc[u] = reinterpret_cast<const float2 *>(scales)[from[u] / LPR];
+        if constexpr (FOUR) {
+          wk[u].x = reinterpret_cast<const uint32_t *>(kc)[from[u]];
+          wv[u].x = reinterpret_cast<const uint32_t *>(vc)[from[u]];
+          const uint8_t *p = static_cast<const uint8_t *>(scales) + from[u] / LPR * (D / 16) + from[u] % LPR / 4;
+          bk[u] = p[0];
+          bv[u] = p[D / 32];
+        } else {
+          wk[u] = reinterpret_cast<const uint2 *>(kc)[from[u]];
+          wv[u] = reinterpret_cast<const uint2 *>(vc)[from[u]];
+          sc[u] = reinterpret_cast<const float2 *>(scales)[from[u] / LPR];
+        }
       }
 #pragma unroll
     for (int u = 0; u < QU; ++u)
-      if (on[u]) {
+      if (on[u] && FOUR) {
+        put8_e2m1(kpool + to[u], wk[u].x, bk[u]);
+        put8_e2m1(vpool + to[u], wv[u].x, bv[u]);
+      } else if (on[u]) {
         put8(kpool + to[u], wk[u], sc[u].x, code);
         put8(vpool + to[u], wv[u], sc[u].y, code);
       }
@@ -236,8 +294,13 @@ hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const 
                                 static_cast<uint8_t *>(c.k_codes), static_cast<uint8_t *>(c.v_codes), c.scales,
                                 c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), sess_dev, src, dst, n_rows);
   };
-  if (p.kv_dtype == IKV_BF16) c.D == 128 ? go(uint16_t(), k_quant_store<uint16_t, 128>) : go(uint16_t(), k_quant_store<uint16_t, 64>);
-  else c.D == 128 ? go(float(), k_quant_store<float, 128>) : go(float(), k_quant_store<float, 64>);
+  auto of = [&](auto tag, auto eight, auto four) { c.code == IKV_E2M1 ? go(tag, four) : go(tag, eight); };
+  if (p.kv_dtype == IKV_BF16)
+    c.D == 128 ? of(uint16_t(), k_quant_store<uint16_t, 128, false>, k_quant_store<uint16_t, 128, true>)
+               : of(uint16_t(), k_quant_store<uint16_t, 64, false>, k_quant_store<uint16_t, 64, true>);
+  else
+    c.D == 128 ? of(float(), k_quant_store<float, 128, false>, k_quant_store<float, 128, true>)
+               : of(float(), k_quant_store<float, 64, false>, k_quant_store<float, 64, true>);
   return hipGetLastError();
 }
 
@@ -251,8 +314,13 @@ hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const i
                                 c.scales, c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), static_cast<T *>(p.k_pool),
                                 static_cast<T *>(p.v_pool), p.num_slots, sess_dev, src, dst, n_rows);
   };
-  if (p.kv_dtype == IKV_BF16) c.D == 128 ? go(uint16_t(), k_quant_load<uint16_t, 128>) : go(uint16_t(), k_quant_load<uint16_t, 64>);
-  else c.D == 128 ? go(float(), k_quant_load<float, 128>) : go(float(), k_quant_load<float, 64>);
+  auto of = [&](auto tag, auto eight, auto four) { c.code == IKV_E2M1 ? go(tag, four) : go(tag, eight); };
+  if (p.kv_dtype == IKV_BF16)
+    c.D == 128 ? of(uint16_t(), k_quant_load<uint16_t, 128, false>, k_quant_load<uint16_t, 128, true>)
+               : of(uint16_t(), k_quant_load<uint16_t, 64, false>, k_quant_load<uint16_t, 64, true>);
+  else
+    c.D == 128 ? of(float(), k_quant_load<float, 128, false>, k_quant_load<float, 128, true>)
+               : of(float(), k_quant_load<float, 64, false>, k_quant_load<float, 64, true>);
   return hipGetLastError();
 }
 

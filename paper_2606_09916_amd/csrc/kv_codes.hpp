@@ -1,5 +1,5 @@
-// 8-bit codes as bf16 matrix operands. Both codes are exact in bf16: an int8 has 7
-// significant bits, an E4M3 value 4.
+// 8-bit and 4-bit codes as bf16 matrix operands. All are exact in bf16: an int8 has 7
+// significant bits, an E4M3 value 4, an E2M1 value 2, and a power of two changes none.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -28,6 +28,27 @@ __device__ __forceinline__ uint2 e4m3_scaled4(uint32_t w, float scale) {
   return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
 }
+
+// 8 adjacent E2M1 codes of a word times a power of two (NaN for an exponent of 255) -> 8 bf16, exactly.
+__device__ __forceinline__ uint4 e2m1_scaled8(uint32_t w, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+}
+
+// The codes of a word whose values with scale byte `e` are not finite, all four bits of each: 4 and 6
+// with 253, 2 and more with 254, all with 255.
+__device__ __forceinline__ uint32_t e2m1_odd(uint32_t w, uint32_t e) {
+  const uint32_t m = e == 255u ? 0x44444444u : e == 254u ? w & 0x44444444u : e == 253u ? w & (w << 1) & 0x44444444u : 0u;
+  return (m >> 2) * 15u;
+}
+
+// Byte i of a word of scale bytes, as its power of two.
+__device__ __forceinline__ float scale_byte(uint32_t w, int i) { return __uint_as_float((w >> (8 * i) & 255u) << 23); }
+
+// Whether some byte of a word is 253 or more.
+__device__ __forceinline__ bool scales_odd(uint32_t w) { return ((((w & 0x7f7f7f7fu) + 0x03030303u) & w) & 0x80808080u) != 0; }
 
 // Whether a scale is anything but a normal power of two: those are 0 .. 253 once the exponent is
 // rotated down, less one; a mantissa, a sign, zero and what is not finite lie above.

@@ -14,7 +14,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libikv.so")
 
 IKV_BF16, IKV_F32 = 0, 1
-IKV_INT8, IKV_E4M3 = 0, 1
+IKV_INT8, IKV_E4M3, IKV_E2M1 = 0, 1, 4
 IKV_RESIDUAL, IKV_NO_XATTN, IKV_POOL7, IKV_TWO_PASS = 1, 2, 4, 8
 CALL_SCORE, CALL_SELECT, CALL_REDIRECT, CALL_DECODE, CALL_COMPACT, CALL_PREFILL, CALL_CHUNK = 1, 2, 3, 4, 5, 6, 7
 STATUS = {0: "IKV_OK", -1: "IKV_EINVAL", -2: "IKV_ESHAPE", -3: "IKV_EWORKSPACE", -4: "IKV_EUNSUPPORTED",
@@ -26,7 +26,7 @@ SYMBOLS = ("ikv_init_dead_slot", "ikv_qm_update", "ikv_score_history", "ikv_sele
            "ikv_timing", "ikv_timing_read", "ikv_memstore_create", "ikv_memstore_destroy", "ikv_memstore_acquire",
            "ikv_memstore_release", "ikv_memstore_trigger", "ikv_memstore_size", "ikv_resolve_span",
            "ikv_compact_apply", "ikv_prefill_span", "ikv_quant_store", "ikv_quant_load", "ikv_decode_attend_quant",
-           "ikv_attend_chunk", "ikv_attend_chunk_quant", "ikv_quant_workspace_bytes")
+           "ikv_attend_chunk", "ikv_attend_chunk_quant", "ikv_quant_workspace_bytes", "ikv_return_slots", "ikv_take_slots")
 IKV_KEY_EXPLICIT, IKV_KEY_SPAN, IKV_KEY_PREFIX, IKV_KEY_LOCAL = 1, 2, 3, 4
 
 
@@ -46,6 +46,11 @@ class QuantPool(ctypes.Structure):
     _fields_ = [("L", c_int32), ("Hq", c_int32), ("Hkv", c_int32), ("D", c_int32),
                 ("num_slots", c_int64), ("dead_slot", c_int32), ("code", c_int32), ("io_dtype", c_int32),
                 ("reserved", c_int32), ("k_codes", c_void_p), ("v_codes", c_void_p), ("scales", c_void_p)]
+
+
+class FreeSlots(ctypes.Structure):
+    _fields_ = [("num_slots", c_int64), ("dead_slot", c_int32), ("reserved", c_int32), ("slots", c_void_p),
+                ("count", c_void_p)]
 
 
 class Session(ctypes.Structure):
@@ -70,6 +75,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2606_09916_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
         P, S, Q = ctypes.POINTER(Pool), ctypes.POINTER(Session), ctypes.POINTER(QuantPool)
+        F = ctypes.POINTER(FreeSlots)
         sig = {
             "ikv_init_dead_slot": [P, c_void_p],
             "ikv_qm_update": [P, S, c_void_p, c_int32, c_void_p, c_void_p, c_float, c_void_p],
@@ -98,6 +104,9 @@ def lib() -> ctypes.CDLL:
             "ikv_attend_chunk_quant": [Q, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
                                        c_void_p, c_void_p, c_size_t, c_void_p],
             "ikv_quant_workspace_bytes": [Q, S, c_int32, c_int32, ctypes.POINTER(c_size_t)],
+            "ikv_return_slots": [F, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p],
+            "ikv_take_slots": [F, S, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                               c_void_p, c_void_p],
             "ikv_timing": [c_int32],
             "ikv_memstore_create": [c_int32, ctypes.POINTER(c_void_p)],
             "ikv_memstore_acquire": [c_void_p, ctypes.POINTER(KeySource), ctypes.POINTER(c_int32),
@@ -173,27 +182,42 @@ def make_pool(k_pool, v_pool, L, Hq, Hkv, D, num_slots, dead_slot=0) -> Pool:
 
 
 def make_quant_pool(k_codes, v_codes, scales, L, Hq, Hkv, D, num_slots, dead_slot=0, io_dtype=None) -> QuantPool:
-    """8-bit cache descriptor over device tensors, which the caller keeps: codes [L][num_slots][Hkv][D] (int8 or float8_e4m3fn), scales
-    [L][num_slots][Hkv][2] float32 (K's, V's). io_dtype: q and out of the attention calls, bfloat16 (the default) or
-    float32."""
+    """Descriptor of a quantised cache over device tensors, which the caller keeps. 8 bits: codes [L][num_slots][Hkv][D]
+    (int8 or float8_e4m3fn), scales [L][num_slots][Hkv][2] float32 (K's, V's). 4 bits (E2M1): codes
+    [L][num_slots][Hkv][D / 2] uint8, two a byte, scales [L][num_slots][Hkv][2][D / 32] uint8. io_dtype: q and out of the
+    attention calls, bfloat16 (the default) or float32."""
     import torch
-    code = {torch.int8: IKV_INT8, torch.float8_e4m3fn: IKV_E4M3}.get(k_codes.dtype)
+    code = {torch.int8: IKV_INT8, torch.float8_e4m3fn: IKV_E4M3, torch.uint8: IKV_E2M1}.get(k_codes.dtype)
     io = {None: IKV_BF16, torch.bfloat16: IKV_BF16, torch.float32: IKV_F32}.get(io_dtype)
     what = "make_quant_pool"
     if code is None:
-        raise IkvError(-1, what, f"codes of type {k_codes.dtype} (int8 or float8_e4m3fn)")
+        raise IkvError(-1, what, f"codes of type {k_codes.dtype} (int8, float8_e4m3fn or uint8)")
     if io is None:
         raise IkvError(-1, what, f"io_dtype {io_dtype} (bfloat16 or float32)")
-    rows = L * num_slots * Hkv
-    _tensor(k_codes, k_codes.dtype, rows * D, what, "k_codes")
-    _tensor(v_codes, k_codes.dtype, rows * D, what, "v_codes")
-    _tensor(scales, torch.float32, rows * 2, what, "scales")
+    rows, four = L * num_slots * Hkv, code == IKV_E2M1
+    _tensor(k_codes, k_codes.dtype, rows * D // (2 if four else 1), what, "k_codes")
+    _tensor(v_codes, k_codes.dtype, rows * D // (2 if four else 1), what, "v_codes")
+    _tensor(scales, torch.uint8 if four else torch.float32, rows * (2 * (D // 32) if four else 2), what, "scales")
     if not k_codes.device == v_codes.device == scales.device:
         raise IkvError(-1, what, "codes and scales on different devices")
     c = QuantPool(L, Hq, Hkv, D, num_slots, dead_slot, code, io, 0, k_codes.data_ptr(), v_codes.data_ptr(),
                   scales.data_ptr())
     c.device = k_codes.device
     return c
+
+
+def make_free_slots(slots, count, num_slots, dead_slot=0) -> FreeSlots:
+    """Descriptor of a stack of free slots over device tensors, which the caller keeps: slots int32 [num_slots], count
+    int32 [2], the free slots (entries [0, count[0]) of slots) and 0."""
+    import torch
+    what = "make_free_slots"
+    _tensor(slots, torch.int32, num_slots, what, "slots")
+    _tensor(count, torch.int32, 2, what, "count")
+    if slots.device != count.device:
+        raise IkvError(-1, what, "slots and count on different devices")
+    f = FreeSlots(num_slots, dead_slot, 0, slots.data_ptr(), count.data_ptr())
+    f.device = slots.device
+    return f
 
 
 class Sessions:
@@ -336,7 +360,7 @@ def _lists(sess: Sessions, ids, counts, func: str, names) -> None:
 
 
 def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=None, stream=None) -> None:
-    """Quantise rows of a pool into the 8-bit cache: slot src[k] (None: row slot_off + k) of the pool to slot dst[k]."""
+    """Quantise rows of a pool into the quantised cache: slot src[k] (None: row slot_off + k) of the pool to slot dst[k]."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_store", ("src", "dst"))
     st = _place("ikv_quant_store", sess, stream, cache, pool, src, dst, n_rows)
     _check(lib().ikv_quant_store(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
@@ -344,7 +368,7 @@ def quant_store(cache: QuantPool, pool: Pool, sess: Sessions, src, dst, n_rows=N
 
 
 def quant_load(cache: QuantPool, pool: Pool, sess: Sessions, src, dst=None, n_rows=None, stream=None) -> None:
-    """Read rows of the 8-bit cache back: slot src[k] of the cache to slot dst[k] (None: row slot_off + k) of the pool."""
+    """Read rows of the quantised cache back: slot src[k] of the cache to slot dst[k] (None: row slot_off + k) of the pool."""
     _lists(sess, (src, dst), n_rows, "ikv_quant_load", ("src", "dst"))
     st = _place("ikv_quant_load", sess, stream, cache, pool, src, dst, n_rows)
     _check(lib().ikv_quant_load(ctypes.byref(cache), ctypes.byref(pool), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(src),
@@ -370,7 +394,7 @@ def _attend(func: str, cache, sess: Sessions, q, live, n_live, out, ws: Workspac
 
 def decode_attend_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
                         window: int = 0, stream=None) -> None:
-    """One new token per session over the 8-bit cache: q, out [B][L][Hq][D] of the cache's io_dtype."""
+    """One new token per session over the quantised cache: q, out [B][L][Hq][D] of the cache's io_dtype."""
     _attend("ikv_decode_attend_quant", cache, sess, q, live, n_live, out, ws, quant_workspace_bytes(cache, sess, CALL_DECODE),
             sinks, window, sess.B, cache.io_dtype, stream)
 
@@ -384,9 +408,31 @@ def attend_chunk(pool: Pool, sess: Sessions, q, live, n_live, out, ws: Workspace
 
 def attend_chunk_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, ws: Workspace, sinks: int = 0,
                        window: int = 0, stream=None) -> None:
-    """attend_chunk over the 8-bit cache: q, out of the cache's io_dtype."""
+    """attend_chunk over the quantised cache: q, out of the cache's io_dtype."""
     _attend("ikv_attend_chunk_quant", cache, sess, q, live, n_live, out, ws, quant_workspace_bytes(cache, sess, CALL_CHUNK),
             sinks, window, sess.span_tokens, cache.io_dtype, stream)
+
+
+def return_slots(free: FreeSlots, sess: Sessions, lists, n_list, stream=None) -> None:
+    """Push the sessions' lists (n_list[b] entries from slot_off on) onto the stack of free slots, in order."""
+    what = "ikv_return_slots"
+    _lists(sess, (lists,), n_list, what, ("lists",))
+    st = _place(what, sess, stream, free, lists, n_list)
+    _check(lib().ikv_return_slots(ctypes.byref(free), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(lists), _ptr(n_list), st),
+           what)
+
+
+def take_slots(free: FreeSlots, sess: Sessions, n_taken, slot_maps=None, live=None, n_live=None, n_all=None, dst=None,
+               n_new=None, stream=None) -> None:
+    """Slots for the tokens of each session's span (with n_new, as many of them), from the stack of free ones: into the
+    slot map, behind the live list (n_all its length afterwards, may be n_live) and as dst for quant_store."""
+    what = "ikv_take_slots"
+    _lists(sess, (slot_maps, live, dst), n_taken, what, ("slot_maps", "live", "dst"))
+    for n in (n_live, n_all, n_new):
+        _lists(sess, (), n, what, ())
+    st = _place(what, sess, stream, free, n_taken, slot_maps, live, n_live, n_all, dst, n_new)
+    _check(lib().ikv_take_slots(ctypes.byref(free), sess.host_ptr, sess.dev_ptr, sess.B, _ptr(n_new), _ptr(slot_maps),
+                                _ptr(live), _ptr(n_live), _ptr(n_all), _ptr(dst), _ptr(n_taken), st), what)
 
 
 # ----------------------------------------------------------------------------- timing

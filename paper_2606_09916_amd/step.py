@@ -70,7 +70,7 @@ class RetentionStep:
         self.n_live = torch.empty(self.B, dtype=torch.int32, device=device)
         self.out = torch.empty_like(self.q_dec)
         self.ws = ikv.Workspace(device)
-        self.cache = None                        # the 8-bit cache, made by quantise()
+        self.cache = None                        # the quantised cache, made by quantise()
 
     # ---------------------------------------------------------------- calls
     def reset(self):
@@ -100,27 +100,34 @@ class RetentionStep:
         ikv.decode_attend_slotmap(self.pool, self.sess, self.q_dec, self.live, self.n_live, self.out, self.ws)
 
     def quantise(self, code: str = "int8"):
-        """Put the rows of the live slots into an 8-bit cache of the pool's shape ("int8" or "e4m3"), same slots:
-        the decode over it reads half the bytes, and the pool can go. Of the rows as they are now: call it again
-        after each step that changes them."""
+        """Put the rows of the live slots into a quantised cache of the pool's shape ("int8", "e4m3" or, in 4 bits,
+        "e2m1"), same slots: the decode over it reads half the bytes or about a quarter, and the pool can go. Of the
+        rows as they are now: call it again after each step that changes them."""
         import torch
-        ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}.get(code)
+        ct = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn, "e2m1": torch.uint8}.get(code)
         if ct is None:
-            raise ikv.IkvError(-1, "RetentionStep.quantise", f"code {code!r} (\"int8\" or \"e4m3\")")
+            raise ikv.IkvError(-1, "RetentionStep.quantise", f"code {code!r} (\"int8\", \"e4m3\" or \"e2m1\")")
         if self.cache is None or self.k_codes.dtype != ct:
-            shape = (self.L, self.num_slots, self.Hkv, self.D)
-            self.k_codes, self.v_codes = (torch.empty(shape, dtype=ct, device=self.device) for _ in range(2))
-            self.code_scales = torch.empty((*shape[:3], 2), dtype=torch.float32, device=self.device)
+            four = code == "e2m1"
+            shape = (self.L, self.num_slots, self.Hkv)
+            self.k_codes, self.v_codes = (torch.empty((*shape, self.D // 2 if four else self.D), dtype=ct, device=self.device)
+                                          for _ in range(2))
+            self.code_scales = (torch.empty((*shape, 2, self.D // 32), dtype=torch.uint8, device=self.device) if four else
+                                torch.empty((*shape, 2), dtype=torch.float32, device=self.device))
             self.cache = ikv.make_quant_pool(self.k_codes, self.v_codes, self.code_scales, self.L, self.Hq, self.Hkv,
                                              self.D, self.num_slots, self.dead, io_dtype=self.q_dec.dtype)
         ikv.quant_store(self.cache, self.pool, self.sess, self.live, self.live, self.n_live)
 
     def decode_quant(self, sinks: int = 0, window: int = 0):
-        """The decode over the 8-bit cache that ``quantise`` filled."""
+        """The decode over the quantised cache that ``quantise`` filled."""
         if self.cache is None:
-            raise ikv.IkvError(-1, "RetentionStep.decode_quant", "no 8-bit cache yet: call quantise() first")
+            raise ikv.IkvError(-1, "RetentionStep.decode_quant", "no quantised cache yet: call quantise() first")
         ikv.decode_attend_quant(self.cache, self.sess, self.q_dec, self.live, self.n_live, self.out, self.ws,
                                 sinks=sinks, window=window)
+
+    def return_freed(self, free):
+        """Push the slots that ``redirect`` freed onto a stack of free ones (``ikv.make_free_slots``)."""
+        ikv.return_slots(free, self.sess, self.freed, self.n_freed)
 
     def step(self, update_memory: bool = True):
         if update_memory:
