@@ -23,7 +23,7 @@ ARCH = "gfx950"
 
 SOURCES = ["ikv_api.hip", "k_memory.hip", "k_score.hip", "k_score_mfma.hip", "k_score_narrow.hip", "k_residual.hip",
            "k_residual_mfma.hip", "k_select.hip", "k_decode.hip", "k_compact.hip", "k_prefill.hip",
-           "k_quant.hip", "k_attend.hip", "k_attend_few.hip", "k_attend_tile.hip", "k_slots.hip",
+           "k_quant.hip", "k_attend.hip", "k_attend_few.hip", "k_attend_four.hip", "k_attend_tile.hip", "k_slots.hip",
            "ikv_session.cpp"]
 
 FLAGS = [

@@ -46,6 +46,8 @@ struct AttendPlan {
   bool too_large;          // does not fit a launch grid
   bool few;                // every session's rows per KV head fit one 16-row block
   int heads, parts;        // few: adjacent KV heads of a workgroup, waves that share a head's entries
+  bool four;               // few: by k_attend_four
+  bool pair;               // four: a wave takes two adjacent KV heads (heads counts pairs)
   int splits;              // of the entries of a session
   int blocks;              // row blocks per (session, layer, KV head): one (few)
   int rows;                // rows per block in the split state
@@ -80,6 +82,10 @@ inline int64_t attend_fill(int64_t n) { return 100 * n / ((n + CUS - 1) / CUS * 
 // A split's state costs rows (D + 2) floats, written and read: lists are cut no finer than 16
 // entries a row, nor for their unevenness finer than 128 (3 tokens of 5 heads in 4 sessions of
 // 700 to 2500: one split 72, four 79, six 87).
+//  - k_attend_four (p.four) never takes eight waves and fills its round to 90%: one session of 8201,
+//    pairs of heads: (4, 1, 7) 63, (4, 1, 5) 76, (4, 2, 7) 69, (2, 2, 7) 72; 48 layers x 92,300:
+//    (4, 1, 5) 837, (4, 2, 5) 854, (4, 1, 10) 869; 16 sessions of 3000: (4, 1, 2) 373, (4, 1, 1) 400,
+//    (4, 2, 1) 406; 4 tokens of 5 heads in 4 sessions of 800 to 3100, 48 x 4: (4, 1, 4) 67, (4, 1, 1) 104.
 inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t longest, bool uneven) {
   int widest = 4;
   while (Hkv % widest) widest /= 2;
@@ -97,12 +103,12 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
                   most = std::min<int64_t>(DEC_MAX_SPLITS, longest / (finest * p.parts));
     p.splits = 0;
     for (int64_t s = 1; s <= most && !p.splits; ++s)
-      if (attend_fill(units * s) >= (longest / (s * p.parts) >= 4096 ? 95 : 70) && 
+      if (attend_fill(units * s) >= (p.four ? 90 : longest / (s * p.parts) >= 4096 ? 95 : 70) &&
           (!uneven || units * s >= 4 * CUS || longest / (s + 1) < 128 * p.rows))
         p.splits = int(s);
     if ((p.splits && p.splits <= 8) || p.heads == 1) {
       if (!p.splits) p.splits = int(std::max<int64_t>(1, most));
-      if (units * p.splits > CUS && longest / p.splits >= 2048 && p.rows <= FEW_ROWS) p.parts *= 2;
+      if (!p.four && units * p.splits > CUS && longest / p.splits >= 2048 && p.rows <= FEW_ROWS) p.parts *= 2;
       return;
     }
   }
@@ -149,7 +155,9 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
   const int64_t groups = std::max<int64_t>(1, int64_t(a.L) * B);
   if (p.few) {
     p.rows = p.max_n * G;
-    attend_few_shape(p, a.Hkv, groups, longest, B > 1 && 20 * longest * B >= 23 * sum);
+    p.four = a.format == KV_E2M1 && !a.io_f32 && a.D == 128;
+    p.pair = p.four && p.rows <= FEW_ROWS && a.Hkv % 2 == 0;
+    attend_few_shape(p, p.pair ? a.Hkv / 2 : a.Hkv, groups, longest, B > 1 && 20 * longest * B >= 23 * sum);
   } else {
     const int64_t rows = int64_t(p.max_n) * G;
     p.rows = rows <= 128 ? 128 : 256;            // four waves or eight

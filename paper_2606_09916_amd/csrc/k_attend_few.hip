@@ -498,7 +498,9 @@ hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream
   if (a.format == KV_BF16) go_few_d<KV_BF16, uint16_t>(a, p, st);
   else if (a.format == KV_INT8) a.io_f32 ? go_few_d<KV_INT8, float>(a, p, st) : go_few_d<KV_INT8, uint16_t>(a, p, st);
   else if (a.format == KV_E4M3) a.io_f32 ? go_few_d<KV_E4M3, float>(a, p, st) : go_few_d<KV_E4M3, uint16_t>(a, p, st);
-  else a.io_f32 ? go_few_d<KV_E2M1, float>(a, p, st) : go_few_d<KV_E2M1, uint16_t>(a, p, st);
+  else if (p.four) {
+    if (const hipError_t e = launch_attend_four(a, p, st)) return e;
+  } else a.io_f32 ? go_few_d<KV_E2M1, float>(a, p, st) : go_few_d<KV_E2M1, uint16_t>(a, p, st);
   return p.splits > 1 ? launch_attend_merge(a, p, st) : hipGetLastError();
 }
 
