@@ -1,12 +1,16 @@
 // Slots pushed onto, and taken from, the stack of free ones.
 //
 // Both calls lay the sessions' lists end to end: session b's part of the T entries in all starts
-// at the sum of the parts before it. A workgroup scans the sessions' counts, TILE at a time, for
-// T and again for the parts that its share of the entries lies in, and finds the session of an
-// entry by bisection. Bound by a launch and by the chain of loads (sessions and counts, then the
-// stack or list, then the stores): every workgroup repeats the scan rather than wait for one.
-// What the calls change in place (count, n_all over n_live, n_taken over n_new) is written by
-// the workgroup that arrives last, once all have read it: count[1] counts the arrivals.
+// at the sum of the parts before it. A workgroup scans the sessions' counts, a tile at a time, for
+// T and (with more than one tile) again for the parts that its share of the entries lies in, and
+// finds the session of an entry by bisection: no workgroup waits for another one's sums.
+// What the calls change in place (count, n_all over n_live, n_taken over n_new) is written by the
+// workgroup that arrives last, once all have read it: count[1] counts the arrivals.
+// Bound by a launch and the chain of loads (counts, then the stack or list, then the stores): 64
+// sessions' tokens take 2 us each call beside the launch; 2.1 million slots of 64 histories, 51 MB,
+// 24 us for both calls (floor 11). There the arrivals count, 10 ns each: 256 workgroups of 512
+// threads 24.2, 512 of 256 30.2, 1024 of 256 40.1; with one entry of a thread on its way at a time
+// instead of eight, 54.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -15,9 +19,11 @@
 
 namespace ikv {
 
-constexpr int ST = 256;                    // threads per workgroup
+constexpr int ST = 512;                    // threads per workgroup
 constexpr int SLOT_TILE = ST;              // sessions scanned at a time, one a thread
 constexpr int SLOT_SHARE = 1024;           // entries of a workgroup, at least
+constexpr int SLOT_UNROLL = 8;             // entries of a thread on their way at once
+constexpr int SLOT_GRID = 256;             // workgroups, at most
 
 struct SlotsLds {
   int32_t wave[ST / WAVE];
@@ -57,11 +63,36 @@ __device__ __forceinline__ int find_session(const int32_t *start, int i) {
   return lo;
 }
 
-// Whether this workgroup is the last to arrive; all of its reads come before.
-__device__ __forceinline__ bool last_to_arrive(int32_t *count, SlotsLds &s) {
+// Entries [from, to) of the lists laid end to end, of which the tile's sessions (s.start, s.off) hold
+// `count` from `before` on: read(session, place in its part, entry) of SLOT_UNROLL entries a thread, then
+// write(.., value) of each. A thread's entries lie ST apart, mostly in one session.
+template <typename Read, typename Write>
+__device__ __forceinline__ void slots_move(const SlotsLds &s, int before, int count, int from, int to, Read read, Write write) {
+  const int lo = max(from - before, 0), hi = min(to - before, count);
+  for (int i0 = lo + int(threadIdx.x); i0 < hi; i0 += ST * SLOT_UNROLL) {
+    int b[SLOT_UNROLL], value[SLOT_UNROLL];
+#pragma unroll
+    for (int u = 0; u < SLOT_UNROLL; ++u) {
+      const int i = min(i0 + u * ST, hi - 1);
+      b[u] = u > 0 ? b[u - 1] : 0;
+      if (u == 0 || s.start[b[u] + 1] <= i) b[u] = find_session(s.start, i);
+      value[u] = read(b[u], i - s.start[b[u]], before + i);
+    }
+#pragma unroll
+    for (int u = 0; u < SLOT_UNROLL; ++u) {
+      const int i = i0 + u * ST;
+      if (i < hi) write(b[u], i - s.start[b[u]], before + i, value[u]);
+    }
+  }
+}
+
+// Whether this workgroup is the last of `all` to arrive. All of its reads are done by then (their values
+// have been used), which is all that the last one's writes have to wait for: the order needs no fence,
+// and a release here would write each XCD's L2 back once per workgroup.
+__device__ __forceinline__ bool last_to_arrive(int32_t *count, int all, SlotsLds &s) {
   __syncthreads();
   if (threadIdx.x == 0)
-    s.last = gridDim.x == 1 || __hip_atomic_fetch_add(&count[1], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == int(gridDim.x) - 1;
+    s.last = all == 1 || __hip_atomic_fetch_add(&count[1], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
   __syncthreads();
   return s.last != 0;
 }
@@ -71,34 +102,43 @@ __device__ __forceinline__ void leave(int32_t *count, int32_t n_free) {
   __hip_atomic_store(&count[1], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// The grid is sized for lists of N entries each; workgroups that the counts leave without a share
+// end at once. (The counts are not changed by the call, so all workgroups agree on that.)
 __global__ void __launch_bounds__(ST) k_return_slots(ikv_free_slots f, const ikv_session *__restrict__ sess, int B,
                                                      const int32_t *__restrict__ list,
                                                      const int32_t *__restrict__ n_list) {
   __shared__ SlotsLds s;
   const int tid = threadIdx.x;
-  auto part = [&](int b) { return b < B ? max(0, min(n_list[b], sess[b].N)) : 0; };
-  int T = 0, tile_sum;
+  const int64_t n_free = max(0, int(min(int64_t(f.count[0]), f.num_slots)));
+  const bool one = B <= SLOT_TILE;               // one tile: scanned once
+  int n, end = 0, T = 0, tile_sum;
+  auto scan = [&](int b0) __attribute__((always_inline)) {
+    const int b = b0 + tid;
+    n = b < B ? max(0, min(n_list[b], sess[b].N)) : 0;
+    end = block_scan(n, s, &tile_sum);
+  };
   for (int b0 = 0; b0 < B; b0 += SLOT_TILE) {
-    block_scan(part(b0 + tid), s, &tile_sum);
+    scan(b0);
     T += tile_sum;
   }
-  const int64_t n_free = max(0, int(min(int64_t(f.count[0]), f.num_slots)));
-  const int from = int(int64_t(T) * blockIdx.x / gridDim.x), to = int(int64_t(T) * (blockIdx.x + 1) / gridDim.x);
+  const int all = min(int(gridDim.x), max(1, (T + SLOT_SHARE - 1) / SLOT_SHARE));
+  if (int(blockIdx.x) >= all) return;
+  const int from = int(int64_t(T) * blockIdx.x / all), to = int(int64_t(T) * (blockIdx.x + 1) / all);
   int before = 0;
   for (int b0 = 0; b0 < B && before < to; b0 += SLOT_TILE) {
-    const int n = part(b0 + tid), end = block_scan(n, s, &tile_sum);
+    if (!one) scan(b0);
     s.start[tid] = end - n;
     s.off[tid] = b0 + tid < B ? sess[b0 + tid].slot_off : 0;
+    if (tid == 0) s.start[SLOT_TILE] = tile_sum;
     __syncthreads();
-    for (int i = max(from - before, 0) + tid; i < min(to - before, tile_sum); i += ST) {
-      const int b = find_session(s.start, i);
-      const int64_t at = n_free + before + i;
-      if (at < f.num_slots) f.slots[at] = list[s.off[b] + (i - s.start[b])];
-    }
+    slots_move(s, before, tile_sum, from, to, [&](int b, int k, int) { return list[s.off[b] + k]; },
+               [&](int, int, int i, int slot) {
+                 if (n_free + i < f.num_slots) f.slots[n_free + i] = slot;
+               });
     before += tile_sum;
     __syncthreads();
   }
-  if (last_to_arrive(f.count, s) && tid == 0) leave(f.count, int32_t(min(n_free + T, f.num_slots)));
+  if (last_to_arrive(f.count, all, s) && tid == 0) leave(f.count, int32_t(min(n_free + T, f.num_slots)));
 }
 
 struct TakeArgs {
@@ -115,21 +155,27 @@ __global__ void __launch_bounds__(ST) k_take_slots(TakeArgs a) {
   __shared__ SlotsLds s;
   const int tid = threadIdx.x;
   const int n_free = max(0, int(min(int64_t(a.f.count[0]), a.f.num_slots)));
-  // tokens that session b asks for, if its list has room; its live entries
-  auto wanted = [&](int b, int *nl) {
-    *nl = 0;
-    if (b >= a.B) return 0;
-    const ikv_session x = a.sess[b];
-    const int n = a.n_new ? max(0, min(a.n_new[b], x.qe - x.qs)) : x.qe - x.qs;
-    if (!a.live) return n;
-    *nl = max(0, min(a.n_live[b], x.N));
-    return n <= x.N - *nl ? n : 0;
+  const bool one = a.B <= SLOT_TILE;
+  int n, nl, end = 0, tile_sum;
+  // n: tokens that a session asks for, if its list has room; nl: its live entries
+  auto scan = [&](int b0) __attribute__((always_inline)) {
+    const int b = b0 + tid;
+    n = nl = 0;
+    if (b < a.B) {
+      const ikv_session x = a.sess[b];
+      n = a.n_new ? max(0, min(a.n_new[b], x.qe - x.qs)) : x.qe - x.qs;
+      if (a.live) {
+        nl = max(0, min(a.n_live[b], x.N));
+        if (n > x.N - nl) n = 0;
+      }
+    }
+    end = block_scan(n, s, &tile_sum);
   };
-  int sum = 0, tile_sum, T = 0, nl;
+  int sum = 0, T = 0;
   for (int b0 = 0; b0 < a.B; b0 += SLOT_TILE) {
-    const int n = wanted(b0 + tid, &nl), end = sum + block_scan(n, s, &tile_sum);
+    scan(b0);
     // the largest sum that the stack holds is what is served
-    int served = end <= n_free ? end : 0;
+    int served = sum + end <= n_free ? sum + end : 0;
 #pragma unroll
     for (int o = 1; o < WAVE; o <<= 1) served = max(served, __shfl_xor(served, o, WAVE));
     __syncthreads();
@@ -144,27 +190,28 @@ __global__ void __launch_bounds__(ST) k_take_slots(TakeArgs a) {
   const int from = int(int64_t(T) * blockIdx.x / gridDim.x), to = int(int64_t(T) * (blockIdx.x + 1) / gridDim.x);
   int before = 0;
   for (int b0 = 0; b0 < a.B && before < to; b0 += SLOT_TILE) {
-    const int n = wanted(b0 + tid, &nl), end = block_scan(n, s, &tile_sum);
+    if (!one) scan(b0);
     s.start[tid] = end - n;
     s.off[tid] = b0 + tid < a.B ? a.sess[b0 + tid].slot_off : 0;
     s.qs[tid] = b0 + tid < a.B ? a.sess[b0 + tid].qs : 0;
     s.nl[tid] = nl;
+    if (tid == 0) s.start[SLOT_TILE] = tile_sum;
     __syncthreads();
-    for (int i = max(from - before, 0) + tid; i < min(to - before, tile_sum); i += ST) {
-      const int b = find_session(s.start, i), t = i - s.start[b];
-      const int32_t slot = top[before + i];
-      const int64_t off = s.off[b] + t;
-      if (a.slot_maps) a.slot_maps[off + s.qs[b]] = slot;
-      if (a.live) a.live[off + s.nl[b]] = slot;
-      if (a.dst) a.dst[off] = slot;
-    }
+    slots_move(s, before, tile_sum, from, to, [&](int, int, int i) { return top[i]; },
+               [&](int b, int t, int, int slot) {
+                 const int64_t at = s.off[b] + t;
+                 if (a.slot_maps) a.slot_maps[at + s.qs[b]] = slot;
+                 if (a.live) a.live[at + s.nl[b]] = slot;
+                 if (a.dst) a.dst[at] = slot;
+               });
     before += tile_sum;
     __syncthreads();
   }
-  if (!last_to_arrive(a.f.count, s)) return;
+  if (!last_to_arrive(a.f.count, gridDim.x, s)) return;
   sum = 0;
   for (int b0 = 0; b0 < a.B; b0 += SLOT_TILE) {
-    const int b = b0 + tid, n = wanted(b, &nl), end = sum + block_scan(n, s, &tile_sum), got = end <= T ? n : 0;
+    if (!one) scan(b0);
+    const int b = b0 + tid, got = sum + end <= T ? n : 0;
     if (b < a.B) {
       a.n_taken[b] = got;
       if (a.live) a.n_all[b] = nl + got;
@@ -175,7 +222,7 @@ __global__ void __launch_bounds__(ST) k_take_slots(TakeArgs a) {
 }
 
 static unsigned slots_grid(int64_t entries) {
-  return unsigned(std::max<int64_t>(1, std::min<int64_t>(2 * 256, entries / SLOT_SHARE)));
+  return unsigned(std::max<int64_t>(1, std::min<int64_t>(SLOT_GRID, entries / SLOT_SHARE)));
 }
 
 hipError_t launch_return_slots(const ikv_free_slots &f, const ikv_session *sess_dev, int B, int64_t entries,
