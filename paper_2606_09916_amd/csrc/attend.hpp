@@ -61,8 +61,8 @@ inline int64_t attend_bound(const ikv_session &s, bool decode) {
   return decode ? decode_live_bound(s) : std::max<int64_t>(1, s.N);
 }
 
-// How full n > 0 workgroups leave their rounds of one per CU, in percent.
-inline int64_t attend_fill(int64_t n) { return 100 * n / ((n + CUS - 1) / CUS * CUS); }
+// How full n > 0 workgroups leave their rounds of one per CU (or `round` in all), in percent.
+inline int64_t attend_fill(int64_t n, int64_t round = CUS) { return 100 * n / ((n + round - 1) / round * round); }
 
 // Workgroups of the few-rows kernel: `heads` adjacent KV heads (their rows lie side by side, so
 // together the waves read long pieces) times `parts` waves that share a head's entries and join
@@ -124,7 +124,28 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
 //    with five, 270 with eight), or the fewest that fill their rounds to 80% for 256 (n = 64: 616
 //    with one, 553 with two, 527 with three, 545 with five).
 //  - else none: n = 128: 903 with one, 944 with two.
-inline int attend_tile_splits(int64_t wgs, int rows, int blocks, int64_t longest) {
+//  - 4 bits, blocks of 128 rows whose workgroups run two to a CU: up to two blocks per head, of at
+//    least 1024 entries, at most five, the fewest that fill rounds of 512 to 80%, or to 75% beyond the
+//    first round of two blocks. Qwen3-8B over 8253, n = 10: 232 with one, 170 with three, 165 with
+//    five; n = 20: 242, 191, 199; n = 61: 418, 388 with two, 392 with three; half 14B over 8000, n = 12:
+//    156, 132, 113; n = 30: 249, 216 with two, 221 with four; 14B over 5000, n = 45: 287, 315 with two.
+//    Up to 128 workgroups: one to a CU, two where a split keeps 1024 entries. One layer over 8253,
+//    n = 61: 31 with 16, 55 with four, 39 with 32; n = 500: 90 with four, 103 with two.
+inline int attend_tile_splits(int64_t wgs, int rows, int blocks, int64_t longest, bool four) {
+  if (four && wgs <= CUS / 2)
+    return int(std::max<int64_t>(1, std::min<int64_t>(std::max(std::min(CUS / wgs, longest / 256), std::min(2 * CUS / wgs, longest / 1024)),
+                                                      DEC_MAX_SPLITS)));
+  if (four) {
+    if (blocks > 2) return 1;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(5, longest / 1024));
+    const int64_t full = blocks == 2 && wgs > 2 * CUS ? 75 : 80;
+    int64_t best = 1;
+    for (int64_t s = 1; s <= most; ++s) {
+      if (attend_fill(wgs * s, 2 * CUS) > attend_fill(wgs * best, 2 * CUS)) best = s;
+      if (attend_fill(wgs * best, 2 * CUS) >= full) break;
+    }
+    return int(best);
+  }
   if (wgs < CUS) return int(std::max<int64_t>(1, std::min<int64_t>({CUS / wgs, longest / 256, DEC_MAX_SPLITS})));
   if (blocks > 1) return 1;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(5, longest / 1024));
@@ -160,9 +181,13 @@ inline AttendPlan attend_plan(const AttendArgs &a, const ikv_session *sess, int 
     attend_few_shape(p, p.pair ? a.Hkv / 2 : a.Hkv, groups, longest, B > 1 && 20 * longest * B >= 23 * sum);
   } else {
     const int64_t rows = int64_t(p.max_n) * G;
-    p.rows = rows <= 128 ? 128 : 256;            // four waves or eight
+    // four waves or eight. Over 4-bit rows always four, two workgroups a CU: their barriers leave one's
+    // products to the other's vector work, and staging twice costs half of what it does for 8 bits (509
+    // tokens over 8192: 2522 us, 256 rows 2621; 200: 1054 and 1289; 61: 388 and 454)
+    const bool four = a.format == KV_E2M1 && !a.io_f32;
+    p.rows = rows <= 128 || four ? 128 : 256;
     p.blocks = int(std::min<int64_t>((rows + p.rows - 1) / p.rows, INT32_MAX));
-    p.splits = attend_tile_splits(groups * a.Hkv * p.blocks, p.rows, p.blocks, longest);
+    p.splits = attend_tile_splits(groups * a.Hkv * p.blocks, p.rows, p.blocks, longest, four);
   }
   // the workspace is sized without the window
   if (window) p.splits = std::min(p.splits, attend_plan(a, sess, B, decode, 0, 0).splits);

@@ -348,9 +348,10 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       // order that the fences keep: NP products of the next tile's logits, then, by turns, one of
       // them and one of step st - 1's values, then the last step's values. Operands are read from
       // LDS AHEAD products before their own. (509 tokens over 8192 entries, int8: 2739 us; in the
-      // compiler's own order 2824.) Four waves with twice the pieces each, and float32's three
-      // parts, have no registers for operands ahead: there the compiler orders them.
-      constexpr bool FENCES = NW == 8 && QP == 1;
+      // compiler's own order 2824; 4 bits, four waves, 1021 tokens, window 4096: 4170, 4340.) Four waves
+      // with twice the pieces each, and float32's three parts, have no registers for operands ahead:
+      // there the compiler orders them.
+      constexpr bool FENCES = (NW == 8 || FMT == KV_E2M1) && QP == 1;
       constexpr int NP = D / 32, OPS = 8 * NP, AHEAD = FENCES ? 2 : 0;
       auto is_first = [](int n) { return n < NP || (n < 7 * NP && (n - NP) % 2 == 0); };
       auto first_of = [](int n) { return n < NP ? n : NP + (n - NP) / 2; };
