@@ -11,9 +11,13 @@
 // wave the registers spill (6.0 ms).
 //   staging   rows or codes go from HBM through registers, are made bf16 (exactly:
 //             int8 codes as they are, E4M3 ones with their scales where those are powers of two,
-//             as the store writes them; with another scale the product is rounded to bf16) and
-//             written to one of two LDS buffers, the keys a tile before the values: keys
-//             [64][D + 8], values [64][D + 32], strides that spread the reads over all banks
+//             as the store writes them; with another scale the product is rounded to bf16; E2M1 ones
+//             with their blocks' scales) and
+//             written to one of two LDS buffers, the keys a tile before the values: rows of D + 8,
+//             entry 16 i + 4 j + k in row 16 i + 4 k + j. Pieces of adjacent rows, as they are written,
+//             then lie in different banks, and so do the 16 rows that a product reads of the keys and
+//             the 4 entries, 4 rows apart, that it reads of the values (4 bits, whose 16 lanes write 4
+//             rows: 4375 -> 4250 us in the case below; the others, bit for bit, as fast as before)
 //   S^T = K Q^T with 32 x 32 x 16 products: lane (h, c) holds entries 8 i + 4 h + (0..3) of
 //             row c, so a row's softmax is two lanes' business
 //   softmax   a reference per row that moves only when a logit is TILE_SLACK above it (the
@@ -27,6 +31,9 @@
 // outputs take queries and weights as three bf16 parts, which at D = 128 do not fit the
 // registers: 42 to 67 of a lane's are spilled (8 layers, 200 tokens over 4000: 340 to 377 us). Of the
 // bf16 outputs' instances, int8 with eight waves, and bf16 rows and E4M3 with four, spill two.
+// 4 bits, 14B, 1021 tokens, window 4096, 4.12 TFLOP: 4.20 ms, 0.98 PFLOP/s: as bf16 rows, since the
+// reads do not bound it. Keys as codes in LDS, made bf16 before each product, take 1% longer (a third
+// of the LDS reads less, a third of the vector work more), 64 rows a wave in 512 registers 9.0 ms.
 #include <math.h>
 
 #include <type_traits>
@@ -61,21 +68,24 @@ __device__ __forceinline__ void tile_parts(const float *x, bf16x8_k (&o)[PARTS])
   }
 }
 
+// The LDS row of a tile's entry, and the entry of a row.
+__device__ __forceinline__ int tile_place(int e) { return (e & ~15) | (e & 3) << 2 | (e >> 2 & 3); }
+
 template <int FMT, typename IO, int D, int NW, bool O32>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
   constexpr int RB = kv_row_bytes(FMT, D);
   constexpr int NT = 64 * NW, ROWS = 32 * NW;
   constexpr int KS = D / 16, DB = D / 32;
-  constexpr int KROW = D + 8, VROW = D + 32;
+  constexpr int ROW = D + 8;                      // bf16 of a row in LDS, 16 bytes past a multiple of the banks
   constexpr int PB = RB < 64 ? 8 : 16;           // bytes of a piece
   constexpr int PPR = RB / PB;                   // pieces of a row
   constexpr int PIECES = TILE_KEYS * PPR;        // of a tile's keys (as many of its values)
   constexpr int PP_ = PIECES > NT ? PIECES / NT : 1;       // pieces of keys, and of values, of a thread
   constexpr int QP = sizeof(IO) == 4 ? 3 : 1, PP = QP;
   static_assert(PIECES % NT == 0 || 2 * PIECES == NT, "whole pieces, or one of keys or values a thread");
-  __shared__ __align__(16) uint16_t ks_[2][TILE_KEYS * KROW];
-  __shared__ __align__(16) uint16_t vs_[2][TILE_KEYS * VROW];
+  __shared__ __align__(16) uint16_t ks_[2][TILE_KEYS * ROW];
+  __shared__ __align__(16) uint16_t vs_[2][TILE_KEYS * ROW];
   __shared__ __align__(16) float sc_[2][2][TILE_KEYS];               // scales: keys' (times log2 e / sqrt D), values'
 
   // units (session, layer, KV head) in steps of 8, so that a unit's blocks and splits run on
@@ -157,18 +167,19 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       v = max(0, min(v, T - 1));                   // past the end the last one again, masked
       return v < first ? v : v + gap;
     };
-    const int key0 = tid % PIECES / PPR;           // of the thread's first piece; each next one NT / PPR on
+    const int key0 = tid % PIECES / PPR;           // LDS row of the thread's first piece; each next one NT / PPR on
+    const int at0 = tile_place(key0);              // and its entry within the tile
     auto slots = [&](int tile) __attribute__((always_inline)) {
       Slots x;
       const int va = tile * TILE_KEYS;
       if (va >= first && va + TILE_KEYS <= T) {
         const int32_t *at = list + (va + gap);
 #pragma unroll
-        for (int i = 0; i < PP_; ++i) x.s[i] = at[key0 + i * (NT / PPR)];
+        for (int i = 0; i < PP_; ++i) x.s[i] = at[at0 + i * (NT / PPR)];
         if constexpr (FMT == KV_INT8) x.sc = at[lane];
       } else {
 #pragma unroll
-        for (int i = 0; i < PP_; ++i) x.s[i] = list[entry(va + key0 + i * (NT / PPR))];
+        for (int i = 0; i < PP_; ++i) x.s[i] = list[entry(va + at0 + i * (NT / PPR))];
         if constexpr (FMT == KV_INT8) x.sc = list[entry(va + lane)];
       }
       return x;
@@ -273,8 +284,8 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
       for (int i = 0; i < PP_; ++i) {
         const int key = key0 + i * (NT / PPR);
-        if (takes_k) put(&ks_[par ^ 1][key * KROW + at], r.k[i], r.ks[i], false);
-        if (takes_v) put(&vs_[par][key * VROW + at], r.v[i], r.vs[i], look);
+        if (takes_k) put(&ks_[par ^ 1][key * ROW + at], r.k[i], r.ks[i], false);
+        if (takes_v) put(&vs_[par][key * ROW + at], r.v[i], r.vs[i], look);
       }
       if constexpr (FMT == KV_INT8) {
         if (tid < TILE_KEYS) {
@@ -290,7 +301,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     auto first_product = [&](Logits &x, int par, int ks) __attribute__((always_inline)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const bf16x8_k kf = *reinterpret_cast<const bf16x8_k *>(&ks_[par][(32 * kb + c) * KROW + 8 * h2 + 16 * ks]);
+        const bf16x8_k kf = *reinterpret_cast<const bf16x8_k *>(&ks_[par][(32 * kb + tile_place(c)) * ROW + 8 * h2 + 16 * ks]);
 #pragma unroll
         for (int p = QP - 1; p >= 0; --p) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][p], x[kb], 0, 0, 0);
       }
@@ -357,15 +368,15 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
       auto first_of = [](int n) { return n < NP ? n : NP + (n - NP) / 2; };
       auto second_of = [](int n) { return n < 7 * NP ? (n - NP) / 2 : n - 4 * NP; };
       const int lr = lane & 15;
-      const uint16_t *kr = &ks_[par ^ 1][c * KROW + 8 * h2];
-      const uint16_t *vr = &vs_[par][(4 * h2 + (lr >> 2)) * VROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3)];
+      const uint16_t *kr = &ks_[par ^ 1][tile_place(c) * ROW + 8 * h2];
+      const uint16_t *vr = &vs_[par][(4 * (lr >> 2) + h2) * ROW + 16 * (lane >> 4 & 1) + 4 * (lr & 3)];
       auto operand = [&](int n) __attribute__((always_inline)) {
         if (is_first(n)) {
           const int q = first_of(n);
-          return *reinterpret_cast<const uint4 *>(kr + 32 * (q & 1) * KROW + 16 * (q >> 1));
+          return *reinterpret_cast<const uint4 *>(kr + 32 * (q & 1) * ROW + 16 * (q >> 1));
         }
         const int q = second_of(n), st = q / NP, db = q % NP;
-        const uint2 x0 = read_tr16(vr + 16 * st * VROW + 32 * db), x1 = read_tr16(vr + (16 * st + 8) * VROW + 32 * db);
+        const uint2 x0 = read_tr16(vr + 16 * st * ROW + 32 * db), x1 = read_tr16(vr + (16 * st + 2) * ROW + 32 * db);
         return make_uint4(x0.x, x0.y, x1.x, x1.y);
       };
       uint4 f[AHEAD + 1];
