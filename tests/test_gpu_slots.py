@@ -77,7 +77,10 @@ TAKE = [([5], [(2, 5)], None, [1], 10), ([5], [(2, 5)], None, [1], 3), ([5], [(2
         ([9] * 5, [(4, 9)] * 5, [2, 0, 5, -3, 99], [3, 9, 5, 4, -1], 30), ([9] * 5, [(4, 9)] * 5, [2, 0, 5, 1, 1], [3, 1, 4, 99, 2], 7),
         ([4] * 600, [(2, 4)] * 600, [1, 2, 0] * 200, [0, 1, 2] * 200, 500), ([3000, 5, 2000], [(0, 3000), (1, 5), (300, 2000)], None,
                                                                              [0, 1, 30], 4705),
-        ([257] * 513, [(1, 257)] * 513, None, [1] * 513, 256 * 500 + 3)]
+        ([257] * 513, [(1, 257)] * 513, None, [1] * 513, 256 * 500 + 3),
+        # several tiles of sessions and several workgroups, counts on the GPU, idle and full sessions among them
+        ([60] * 1300, [(20, 60)] * 1300, [40, 0, 17, 99, 1] * 260, [5, 60, 21, 20, 59, 0, 30, 61, -2, 44] * 130, 20000),
+        ([60] * 1300, [(20, 60)] * 1300, [40, 0, 17, 99, 1] * 260, [5, 20, 21, 20, 59, 0, 13, 1, -2, 4] * 130, 90000)]
 
 
 @pytest.mark.parametrize("Ns,spans,n_new,n_live,have", TAKE)
