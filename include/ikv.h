@@ -457,7 +457,7 @@ ikv_status ikv_prefill_span(const ikv_pool *pool, const ikv_session *sess,
  *   k_codes, v_codes: device, [L][num_slots][Hkv][D / 2] bytes, 16-byte aligned; channel 2 i
  *           in the low four bits of byte i, channel 2 i + 1 in the high ones. A code is a sign
  *           (bit 3) and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0 to 2).
- *   scales: device bytes, [L][num_slots][Hkv][2][D / 32], 8-byte aligned: of the K row's
+ *   scales: device bytes, [L][num_slots][Hkv][2][D / 32], D/16-byte aligned: of the K row's
  *           blocks, then of the V row's. Byte e is the scale 2^(e - 127), 255 is NaN.
  * With a = max(max_d |x_d|, 2^-100) over the block the store writes
  *   scale = the least power of two with 7 scale >= a, but at most 2^125 (bytes 25 .. 252);
@@ -613,7 +613,8 @@ ikv_status ikv_return_slots(const ikv_free_slots *free_slots, const ikv_session 
  *   n_all: device int32 [B]: the live list's length afterwards, of every session; may be n_live.
  * Nothing else is written. n_taken may be n_new. Otherwise no two arrays may overlap.
  * ikv_return_slots with dst and n_taken puts the slots back as they were.
- * Both calls: at most 2^31 - 1 entries of all sessions together (spans' tokens for the take).
+ * Both calls: at most 2^30 entries of all sessions together (N each; their spans' tokens for the
+ * take; IKV_EUNSUPPORTED).
  */
 ikv_status ikv_take_slots(const ikv_free_slots *free_slots, const ikv_session *sess,
                           const ikv_session *sess_dev, int32_t B, const int32_t *n_new,

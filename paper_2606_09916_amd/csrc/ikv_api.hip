@@ -87,9 +87,10 @@ ikv_status check_quant_pool(const ikv_quant_pool *c) {
   if (c->io_dtype != IKV_BF16 && c->io_dtype != IKV_F32) return fail(IKV_EINVAL, "cache: unknown io_dtype %d", c->io_dtype);
   if (c->reserved != 0) return fail(IKV_EINVAL, "cache: reserved must be 0");
   if (!c->k_codes || !c->v_codes || !c->scales) return fail(IKV_EINVAL, "cache: k_codes / v_codes / scales is NULL");
+  const int scale_bytes = c->code == IKV_E2M1 ? c->D / 16 : 8;       // of a slot and head
   if ((reinterpret_cast<uintptr_t>(c->k_codes) | reinterpret_cast<uintptr_t>(c->v_codes)) % 16 ||
-      reinterpret_cast<uintptr_t>(c->scales) % 8)
-    return fail(IKV_EINVAL, "cache: k_codes and v_codes must be 16-byte aligned, scales 8-byte aligned");
+      reinterpret_cast<uintptr_t>(c->scales) % scale_bytes)
+    return fail(IKV_EINVAL, "cache: k_codes and v_codes must be 16-byte aligned, scales %d-byte aligned", scale_bytes);
   return IKV_OK;
 }
 
@@ -856,7 +857,7 @@ ikv_status ikv_return_slots(const ikv_free_slots *free_slots, const ikv_session 
   if (!list || !n_list) return fail(IKV_EINVAL, "list / n_list is NULL");
   int64_t entries = 0;
   for (int b = 0; b < B; ++b) entries += sess[b].N;
-  if (entries > INT32_MAX) return fail(IKV_EUNSUPPORTED, "ikv_return_slots: more than 2^31 - 1 entries");
+  if (entries > ikv::SLOTS_MOST) return fail(IKV_EUNSUPPORTED, "ikv_return_slots: more than 2^30 entries");
   if (debug_mode()) {
     const hipStream_t st = (hipStream_t)stream;
     std::vector<bool> used;
@@ -892,7 +893,7 @@ ikv_status ikv_take_slots(const ikv_free_slots *free_slots, const ikv_session *s
   if (!live != !n_live || !live != !n_all) return fail(IKV_EINVAL, "live, n_live and n_all must be given together");
   int64_t tokens = 0;
   for (int b = 0; b < B; ++b) tokens += sess[b].qe - sess[b].qs;
-  if (tokens > INT32_MAX) return fail(IKV_EUNSUPPORTED, "ikv_take_slots: more than 2^31 - 1 tokens");
+  if (tokens > ikv::SLOTS_MOST) return fail(IKV_EUNSUPPORTED, "ikv_take_slots: more than 2^30 tokens");
   if (debug_mode()) {
     std::vector<bool> used;
     int32_t n_free = 0;

@@ -333,6 +333,7 @@ hipError_t launch_attend_tile(const AttendArgs &a, const AttendPlan &p, hipStrea
 hipError_t launch_attend_merge(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 
+constexpr int64_t SLOTS_MOST = int64_t(1) << 30;   // entries of all sessions in a call on the stack of free slots
 hipError_t launch_return_slots(const ikv_free_slots &f, const ikv_session *sess_dev, int B, int64_t entries,
                                const int32_t *list, const int32_t *n_list, hipStream_t st);
 hipError_t launch_take_slots(const ikv_free_slots &f, const ikv_session *sess_dev, int B, int64_t tokens,

@@ -488,7 +488,9 @@ static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
 
 template <int FMT, typename IO>
 static void go_few_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if constexpr (FMT != KV_BF16 && sizeof(IO) == 2) {
+  if constexpr (FMT == KV_E2M1 && sizeof(IO) == 2) {             // D = 128: k_attend_four
+    return p.rows > 16 ? go_few<FMT, IO, 64, 2>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
+  } else if constexpr (FMT != KV_BF16 && sizeof(IO) == 2) {
     if (p.rows > 16) return a.D == 128 ? go_few<FMT, IO, 128, 2>(a, p, st) : go_few<FMT, IO, 64, 2>(a, p, st);
   }
   a.D == 128 ? go_few<FMT, IO, 128, 1>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);

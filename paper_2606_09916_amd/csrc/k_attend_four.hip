@@ -29,13 +29,6 @@ namespace ikv {
 constexpr float FOUR_SLACK = 8.f;                // log2: as in k_attend_few.hip
 constexpr int FOUR_BLOCK = 32;                   // entries per block
 constexpr int FOUR_ROW = 136;                    // bf16 of a value row in LDS
-typedef short s16x4_four __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ uint2 four_tr16(const uint16_t *p) {
-  return __builtin_bit_cast(
-      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_four *)p));
-}
-
 // The place of an entry's value row among 16. Rows lie 17 pieces of 16 bytes apart: the same piece of
 // 16 rows, as it is written, lies in 16 different ones of the LDS's 256 bytes of banks, and two adjacent
 // pieces of entries 0 .. 7 or 8 .. 15, as half a wave reads them, do not overlap there.
@@ -273,7 +266,7 @@ k_attend_four(AttendArgs a, int heads, int rows_max) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint16_t *from = vget + h * (VALUES / 2) + 16 * t;
-          const uint2 x0 = four_tr16(from), x1 = four_tr16(from + 16 * FOUR_ROW);
+          const uint2 x0 = read_tr16(from), x1 = read_tr16(from + 16 * FOUR_ROW);
           const bf16x8_k vf = __builtin_bit_cast(bf16x8_k, make_uint4(x0.x, x0.y, x1.x, x1.y));
 #pragma unroll
           for (int p = PP - 1; p >= 0; --p)
@@ -419,16 +412,18 @@ static void go_four(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
     k_attend_four<NH, ROWS, NW, false><<<grid, WAVE * NW, 0, st>>>(a, p.heads, p.rows);
 }
 
+// Up to 16 rows.
 template <int NW> static void go_four_w(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if (p.rows > 16) go_four<1, 32, NW>(a, p, st);
-  else if (p.rows > 8) p.pair ? go_four<2, 16, NW>(a, p, st) : go_four<1, 16, NW>(a, p, st);
+  if (p.rows > 8) p.pair ? go_four<2, 16, NW>(a, p, st) : go_four<1, 16, NW>(a, p, st);
   else p.pair ? go_four<2, 8, NW>(a, p, st) : go_four<1, 8, NW>(a, p, st);
 }
 
 hipError_t launch_attend_four(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   KTimer kt_("k_attend_four", st);
-  if (p.heads * p.parts == 8) go_four_w<8>(a, p, st);
-  else if (p.heads * p.parts == 4) go_four_w<4>(a, p, st);
+  const int waves = p.heads * p.parts;
+  if (p.rows > 16 && waves == 4) go_four<1, 32, 4>(a, p, st);
+  else if (p.rows <= 16 && waves == 8) go_four_w<8>(a, p, st);
+  else if (p.rows <= 16 && waves == 4) go_four_w<4>(a, p, st);
   else return hipErrorInvalidConfiguration;
   return hipGetLastError();
 }

@@ -45,14 +45,8 @@
 namespace ikv {
 
 typedef float f32x16_k __attribute__((ext_vector_type(16)));
-typedef short s16x4_k __attribute__((ext_vector_type(4)));
 
 constexpr float TILE_SLACK = 8.f;                // log2
-
-__device__ __forceinline__ uint2 read_tr16(const uint16_t *p) {
-  return __builtin_bit_cast(
-      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_k *)p));
-}
 
 // 8 floats as PARTS bf16 operands (nearest, then the nearest of what is left).
 template <int PARTS>
@@ -560,7 +554,8 @@ static void go_tile(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
 
 template <int FMT, typename IO>
 static hipError_t go_tile_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-  if (a.D == 128) p.rows == 256 ? go_tile<FMT, IO, 128, 8>(a, p, st) : go_tile<FMT, IO, 128, 4>(a, p, st);
+  if constexpr (FMT == KV_E2M1 && sizeof(IO) == 2) a.D == 128 ? go_tile<FMT, IO, 128, 4>(a, p, st) : go_tile<FMT, IO, 64, 4>(a, p, st);
+  else if (a.D == 128) p.rows == 256 ? go_tile<FMT, IO, 128, 8>(a, p, st) : go_tile<FMT, IO, 128, 4>(a, p, st);
   else p.rows == 256 ? go_tile<FMT, IO, 64, 8>(a, p, st) : go_tile<FMT, IO, 64, 4>(a, p, st);
   return p.splits > 1 ? launch_attend_merge(a, p, st) : hipGetLastError();
 }

@@ -33,7 +33,8 @@ struct SlotsLds {
   int32_t last;
 };
 
-// Inclusive sums over the workgroup; *total of all. Counts sum to less than 2^31.
+// Inclusive sums over the workgroup; *total of all. Counts sum to at most SLOTS_MOST: entry numbers stay in
+// 32 bits, a round of the workgroup's threads past the last one too.
 __device__ __forceinline__ int block_scan(int x, SlotsLds &s, int *total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll

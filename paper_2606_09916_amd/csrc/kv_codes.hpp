@@ -89,6 +89,14 @@ template <int FMT> __device__ __forceinline__ void codes_across(uint32_t a, uint
   }
 }
 
+// The transposing LDS read: 16 lanes read 4 rows of 16 bf16, 8 bytes each (row lane / 4), and get 4 rows
+// of one column each.
+typedef short s16x4_k __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 read_tr16(const uint16_t *p) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_k *)p));
+}
+
 // bf16 values that are not finite, by pairs. Zero weights of rows that do not see an entry would
 // turn them into NaN, so where some row does not, the product takes the pair without them, and
 // they are added afterwards to the sums of the rows that do.

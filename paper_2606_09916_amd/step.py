@@ -127,6 +127,9 @@ class RetentionStep:
 
     def return_freed(self, free):
         """Push the slots that ``redirect`` freed onto a stack of free ones (``ikv.make_free_slots``)."""
+        if (free.num_slots, free.dead_slot) != (self.num_slots, self.dead):
+            raise ikv.IkvError(-1, "RetentionStep.return_freed",
+                               f"free slots of a pool of {free.num_slots} slots (sentinel {free.dead_slot}), not of this one")
         ikv.return_slots(free, self.sess, self.freed, self.n_freed)
 
     def step(self, update_memory: bool = True):

@@ -17,7 +17,7 @@ def _source():
     for old, new in ((WIDTHS, "for (int fmt = 3; fmt < 4; ++fmt) for (int D : {64, 128})"), ("a.D = 128,", "a.D = D,"),
                      ("CHECK(p.heads >= 1 && a.Hkv % p.heads == 0 &&",
                       "CHECK(p.four == (D == 128 && !f32) && (!p.pair || p.four));\n"
-                      "          if (p.four) CHECK((p.heads * p.parts == 4 || p.heads * p.parts == 8) && !(p.pair && p.rows > 16));\n"
+                      "          if (p.four) CHECK((p.heads * p.parts == 4 || (p.heads * p.parts == 8 && p.rows <= 16)) && !(p.pair && p.rows > 16));\n"
                       "          CHECK(p.heads >= 1 && a.Hkv % (p.heads * (p.pair ? 2 : 1)) == 0 &&"),
                      ("CHECK((p.rows == 128 || p.rows == 256) && p.blocks >= 1);",
                       "CHECK((f32 ? p.rows == 128 || p.rows == 256 : p.rows == 128) && p.blocks >= 1);")):

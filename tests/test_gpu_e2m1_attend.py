@@ -54,6 +54,16 @@ def test_chunk_sizes(dev, io, N, n):
         s.check(s.run(q, sinks, window), q, [n], sinks, window)
 
 
+@pytest.mark.parametrize("L,Hq,Hkv", [(1, 4, 1), (2, 7, 1), (1, 24, 3), (3, 6, 3), (2, 8, 2), (40, 10, 5)])
+@pytest.mark.parametrize("n", [1, 2, 4])
+def test_short_lists_of_odd_and_even_heads(dev, L, Hq, Hkv, n):
+    """One KV head a wave (odd numbers of them) or two, eight waves a head or four, 8, 16 and 32 rows."""
+    s = Four(dev, "bf16", L, Hq, Hkv, 128, [400, 257, 300], n, seed=Hq + n)
+    q = s.queries(3 * n)
+    for sinks, window in ((0, 0), (3, 40)):
+        s.check(s.run(q, sinks, window, decode=n == 1), q, [n] * 3, sinks, window)
+
+
 @pytest.mark.parametrize("io", IO)
 def test_ragged_chunks(dev, io):
     s = Four(dev, io, 2, 8, 2, 128, [1, 55, 0, 40], 40)
@@ -110,6 +120,18 @@ def test_unseen_scales_of_nan(dev, io, form):
     assert torch.equal(out[:, ~sees], clean[:, ~sees])
     assert out[:, sees][..., 32 * block:].isnan().all()
     assert torch.equal(out[:, sees][..., :32 * block], clean[:, sees][..., :32 * block])
+
+
+@pytest.mark.parametrize("io,form", FORMS)
+def test_keys_of_nan(dev, io, form):
+    """A key block that stands for NaN spoils the tokens that see it, and no others."""
+    import torch
+
+    def change(s, hidden, some):
+        s.sc[:, some if len(some) else hidden, :, 0, 1] = 255
+
+    clean, out, sees = _runs(dev, io, form, change)
+    assert torch.equal(out[:, ~sees], clean[:, ~sees]) and out[:, sees].isnan().all()
 
 
 @pytest.mark.parametrize("io,form", FORMS)
@@ -262,6 +284,28 @@ def test_a_query_that_is_not_finite_spoils_its_row_only(dev, N, n):
         bad = torch.zeros(4, n, dtype=torch.bool, device=dev)
         bad[2, n // 2] = True
         assert out[bad].isnan().all() and torch.equal(out[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_layer_of_a_cache_with_an_odd_number_of_slots(dev, D):
+    """Layers whose scales begin at any slot's alignment."""
+    import torch
+    s = Four(dev, "bf16", 3, 4, 1, D, [201], 9)
+    assert s.slots % 2 == 1
+    q = s.queries(9)
+    out = s.run(q).view(3, -1)
+    for l in range(3):
+        one = ikv.make_quant_pool(s.k[l:l + 1], s.v[l:l + 1], s.sc[l:l + 1], 1, 4, 1, D, s.slots, 0)
+        got = torch.empty_like(out[l])
+        ikv.attend_chunk_quant(one, s.sess, q.view(3, -1)[l].clone(), s.live, s.nl, got, ikv.Workspace(dev))
+        assert torch.equal(got, out[l])
+        d = q.view(3, 4, 9, D)[l, :, 0].contiguous().flatten()
+        one_out = torch.empty_like(d)
+        ikv.decode_attend_quant(one, s.sess, d, s.live, s.nl, one_out, ikv.Workspace(dev))
+        k, v = (s.rows(w, l, s.live.long()).numpy() for w in "kv")
+        want, A, X = qo.attend(d.view(4, 1, D).double().cpu().numpy(), k, v)
+        E = ((D + 8) * X + 4 * (1 + X) + 201 + 8) * 2.0 ** -24
+        assert np.all(np.abs(one_out.view(4, 1, D).double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -17 + 2 * E[..., None]) * A)
 
 
 @pytest.mark.parametrize("Hkv,D,slots", [(8, 128, 8_500_000), (1, 64, 17_000_000)])

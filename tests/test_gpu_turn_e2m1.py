@@ -55,6 +55,8 @@ def test_step_quantises_what_it_keeps(dev, D, kv):
     s = Stack([], st.num_slots, dev)
     st.return_freed(s.free)
     assert s() == freed[0] + freed[1] and len(s()) > 0
+    with pytest.raises(ikv.IkvError, match="not of this one"):
+        st.return_freed(Stack([], st.num_slots + 1, dev).free)
     st.quantise("e4m3")
     assert st.k_codes.dtype == torch.float8_e4m3fn
 

@@ -14,10 +14,18 @@ def _four(**kw):
 
 @pytest.mark.parametrize("field,value,code", [
     ("Hq", 7, ESHAPE), ("D", 32, EUNSUPPORTED), ("D", 96, EUNSUPPORTED), ("num_slots", 0, ESHAPE), ("dead_slot", 100, ESHAPE),
-    ("io_dtype", 7, EINVAL), ("k_codes", PTR + 8, EINVAL), ("scales", PTR + 4, EINVAL), ("scales", None, EINVAL)])
+    ("io_dtype", 7, EINVAL), ("k_codes", PTR + 8, EINVAL), ("scales", PTR + 2, EINVAL), ("scales", None, EINVAL)])
 def test_descriptor(field, value, code):
     c = _four(**{field: value})
     assert _store(c) == code and _load(c) == code and _attend("decode", c) == code and _attend("chunk_quant", c) == code
+
+
+def test_scales_alignment():
+    # one slot and head: 4 bytes at D = 64, 8 at D = 128; a layer of an odd number of slots may begin at either
+    empty = _sess(N=0, qs=0, qe=0)
+    assert _store(_four(scales=PTR + 4), s=empty) == 0
+    assert _store(_four(D=128, scales=PTR + 4), _pool(D=128), empty) == EINVAL
+    assert _store(_four(D=128, scales=PTR + 8), _pool(D=128), empty) == 0
 
 
 @pytest.mark.parametrize("code", [2, 3, 5, -1])

@@ -48,12 +48,14 @@ def test_arguments():
     assert _give(B=0, lists=None) == 0 and _take(B=0, n_taken=None) == 0
 
 
-def test_sums_past_31_bits():
+def test_sums_past_the_limit():
     s = (ikv.Session * 2)()
-    for x in s:
-        x.N, x.qe, x.R = 1 << 30, 1 << 30, 1
+    for x, n in zip(s, (1 << 30, 1)):
+        x.N, x.qe, x.R = n, n, 1
     p = ctypes.cast(s, ctypes.POINTER(ikv.Session))
     assert _give(s=p, B=2) == EUNSUPPORTED and _take(s=p, B=2) == EUNSUPPORTED
+    s[0].N = s[0].qe = (1 << 31) - 1
+    assert _give(s=p) == EUNSUPPORTED and _take(s=p) == EUNSUPPORTED
 
 
 def test_binding():
