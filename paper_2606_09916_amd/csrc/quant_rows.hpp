@@ -7,7 +7,7 @@
 namespace ikv {
 
 constexpr int QT = 256;                    // threads per workgroup
-constexpr int QU = 4;                      // places of a thread at a time
+constexpr int QU = 2;                      // places of a thread at a time
 constexpr int QUANT_MOST = (1 << 24) - 1;  // rows of a session in one call: a workgroup or more each, under 2^32 threads
 
 // Entries of a workgroup: QU places per thread, one entry at least. `per` = Hkv D / 8 places an
