@@ -82,7 +82,7 @@ inline int64_t attend_fill(int64_t n, int64_t round = CUS) { return 100 * n / ((
 // A split's state costs rows (D + 2) floats, written and read: lists are cut no finer than 16
 // entries a row, nor for their unevenness finer than 128 (3 tokens of 5 heads in 4 sessions of
 // 700 to 2500: one split 72, four 79, six 87).
-//  - k_attend_four (p.four) never takes eight waves and fills its round to 90%: one session of 8201,
+//  - k_attend_four (p.four) takes four waves for them and fills its round to 90%: one session of 8201,
 //    pairs of heads: (4, 1, 7) 63, (4, 1, 5) 76, (4, 2, 7) 69, (2, 2, 7) 72; 48 layers x 92,300:
 //    (4, 1, 5) 837, (4, 2, 5) 854, (4, 1, 10) 869; 16 sessions of 3000: (4, 1, 2) 373, (4, 1, 1) 400,
 //    (4, 2, 1) 406; 4 tokens of 5 heads in 4 sessions of 800 to 3100, 48 x 4: (4, 1, 4) 67, (4, 1, 1) 104.

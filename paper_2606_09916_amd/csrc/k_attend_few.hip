@@ -147,7 +147,8 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       return list[v < first ? v : v + gap];
     };
     // Value rows go past the caches (nothing reads them again: 123 -> 113 us at 8192 entries); key
-    // rows do not, since two loads of 64 bytes share each of their lines (so: 121).
+    // rows do not, since two loads of 64 bytes share each of their lines (so: 121), and 4-bit ones
+    // neither, whose lines hold other heads' rows.
     auto load = [&](Block &x, int sl) __attribute__((always_inline)) {
       if constexpr (SCALED) x.s = *reinterpret_cast<const float2 *>(sbase + row_at(sl, 0) / (D / 8));     // in the order of use
       else if constexpr (FMT == KV_E2M1 && D == 128) x.s = *reinterpret_cast<const float2 *>(sbase + row_at(sl, 0) / 8);
@@ -166,7 +167,8 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       for (int e = 0; e < 8; ++e) {
         const int at = e < 4 ? 4 * g + e : 16 + 4 * g + e - 4;
         const char *p = vbase + row_at(__builtin_amdgcn_ds_bpermute(4 * at, sl), c * (RB / 16));
-        if constexpr (RB == 32) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t *>(p));
+        if constexpr (RB == 32) x.v[e][0] = *reinterpret_cast<const uint16_t *>(p);
+        else if constexpr (FMT == KV_E2M1) x.v[e][0] = *reinterpret_cast<const uint32_t *>(p);
         else if constexpr (VW == 1) x.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
         else if constexpr (VW == 2) {
           const u32x2_few y = __builtin_nontemporal_load(reinterpret_cast<const u32x2_few *>(p));
@@ -489,11 +491,12 @@ static void go_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
 template <int FMT, typename IO>
 static void go_few_d(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
   if constexpr (FMT == KV_E2M1 && sizeof(IO) == 2) {             // D = 128: k_attend_four
-    return p.rows > 16 ? go_few<FMT, IO, 64, 2>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
+    p.rows > 16 ? go_few<FMT, IO, 64, 2>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
+    return;
   } else if constexpr (FMT != KV_BF16 && sizeof(IO) == 2) {
     if (p.rows > 16) return a.D == 128 ? go_few<FMT, IO, 128, 2>(a, p, st) : go_few<FMT, IO, 64, 2>(a, p, st);
   }
-  a.D == 128 ? go_few<FMT, IO, 128, 1>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
+  if constexpr (FMT != KV_E2M1 || sizeof(IO) == 4) a.D == 128 ? go_few<FMT, IO, 128, 1>(a, p, st) : go_few<FMT, IO, 64, 1>(a, p, st);
 }
 
 hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
