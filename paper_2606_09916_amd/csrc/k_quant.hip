@@ -127,7 +127,7 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
   return n_rows ? max(0, min(n_rows[b], s.N)) : s.N;
 }
 
-// A workgroup takes `group` list entries of one layer; an entry is `per` = Hkv D / 8 threads'
+// A workgroup takes `group` list entries of one layer at a time; an entry is `per` = Hkv D / 8 threads'
 // work, a thread's 8 channels of its K and of its V row. A thread takes QU places at a time,
 // all their slots loaded first, then all their rows: bound by memory, the kernels need that
 // many bytes in flight per CU. 8192 rows of 36 layers x 8 heads, D = 128, bf16, E4M3: stored in
@@ -145,62 +145,64 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
   constexpr int LPR = D / 8;
   const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
   const ikv_session s = sess[b];
-  const int k0 = blockIdx.x * group;
-  const int todo = quant_places(group, quant_rows(s, n_rows, b), k0, per);
-  const int64_t e0 = s.slot_off + k0;
-  for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
-    Row8<T> rk[QU], rv[QU];
-    int64_t to[QU];
-    int at[QU];                                    // place within the entry's row; -1: none
-    int64_t from[QU];
+  const int rows = quant_rows(s, n_rows, b);
+  for (int k0 = blockIdx.x * group; k0 < rows; k0 += gridDim.x * group) {
+    const int todo = quant_places(group, rows, k0, per);
+    const int64_t e0 = s.slot_off + k0;
+    for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
+      Row8<T> rk[QU], rv[QU];
+      int64_t to[QU];
+      int at[QU];                                    // place within the entry's row; -1: none
+      int64_t from[QU];
 #pragma unroll
-    for (int u = 0; u < QU; ++u) {
-      const int i = min(i0 + u * QT, todo - 1), k = i / per;
-      const int64_t e = e0 + k;
-      const int slot = dst[e];
-      at[u] = i0 + u * QT < todo && slot != dead ? i - k * per : -1;
-      to[u] = (int64_t(l) * num_slots + slot) * Hkv;
-      from[u] = ((int64_t(l) * pool_slots + (src ? int64_t(src[e]) : e)) * Hkv) * D + (i - k * per) * 8;
-    }
-#pragma unroll
-    for (int u = 0; u < QU; ++u)
-      if (at[u] >= 0) {
-        rk[u].ld(kpool + from[u]);
-        rv[u].ld(vpool + from[u]);
+      for (int u = 0; u < QU; ++u) {
+        const int i = min(i0 + u * QT, todo - 1), k = i / per;
+        const int64_t e = e0 + k;
+        const int slot = dst[e];
+        at[u] = i0 + u * QT < todo && slot != dead ? i - k * per : -1;
+        to[u] = (int64_t(l) * num_slots + slot) * Hkv;
+        from[u] = ((int64_t(l) * pool_slots + (src ? int64_t(src[e]) : e)) * Hkv) * D + (i - k * per) * 8;
       }
 #pragma unroll
-    for (int u = 0; u < QU; ++u) {
-      if (at[u] < 0) continue;                     // the lanes of a row go together
-      uint2 w[2];
-      float sc[2];
-      uint8_t byte[2];
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        float x[8];
-        (kv ? rv[u] : rk[u]).get(x);
-        uint32_t m = 0;                            // |x| as bits: ordered, a NaN above infinity
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-#pragma unroll
-        for (int o = 1; o < (FOUR ? 4 : LPR); o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
-        if constexpr (FOUR) w[kv].x = quant8_e2m1(x, m, &byte[kv]);
-        else w[kv] = quant8<T>(x, m, code, &sc[kv]);
-      }
-      const int64_t row = to[u] + at[u] / LPR;
-      const int piece = at[u] % LPR;
-      if constexpr (FOUR) {
-        __builtin_nontemporal_store(w[0].x, reinterpret_cast<uint32_t *>(kc + row * (D / 2) + piece * 4));
-        __builtin_nontemporal_store(w[1].x, reinterpret_cast<uint32_t *>(vc + row * (D / 2) + piece * 4));
-        if (piece % 4 == 0) {
-          uint8_t *p = static_cast<uint8_t *>(scales) + row * (D / 16) + piece / 4;
-          p[0] = byte[0];
-          p[D / 32] = byte[1];
+      for (int u = 0; u < QU; ++u)
+        if (at[u] >= 0) {
+          rk[u].ld(kpool + from[u]);
+          rv[u].ld(vpool + from[u]);
         }
-        continue;
+#pragma unroll
+      for (int u = 0; u < QU; ++u) {
+        if (at[u] < 0) continue;                     // the lanes of a row go together
+        uint2 w[2];
+        float sc[2];
+        uint8_t byte[2];
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          float x[8];
+          (kv ? rv[u] : rk[u]).get(x);
+          uint32_t m = 0;                            // |x| as bits: ordered, a NaN above infinity
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+          for (int o = 1; o < (FOUR ? 4 : LPR); o <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), o, WAVE)));
+          if constexpr (FOUR) w[kv].x = quant8_e2m1(x, m, &byte[kv]);
+          else w[kv] = quant8<T>(x, m, code, &sc[kv]);
+        }
+        const int64_t row = to[u] + at[u] / LPR;
+        const int piece = at[u] % LPR;
+        if constexpr (FOUR) {
+          __builtin_nontemporal_store(w[0].x, reinterpret_cast<uint32_t *>(kc + row * (D / 2) + piece * 4));
+          __builtin_nontemporal_store(w[1].x, reinterpret_cast<uint32_t *>(vc + row * (D / 2) + piece * 4));
+          if (piece % 4 == 0) {
+            uint8_t *p = static_cast<uint8_t *>(scales) + row * (D / 16) + piece / 4;
+            p[0] = byte[0];
+            p[D / 32] = byte[1];
+          }
+          continue;
+        }
+        st_past(kc + row * D + piece * 8, w[0]);
+        st_past(vc + row * D + piece * 8, w[1]);
+        if (piece == 0) reinterpret_cast<float2 *>(scales)[row] = make_float2(sc[0], sc[1]);
       }
-      st_past(kc + row * D + piece * 8, w[0]);
-      st_past(vc + row * D + piece * 8, w[1]);
-      if (piece == 0) reinterpret_cast<float2 *>(scales)[row] = make_float2(sc[0], sc[1]);
     }
   }
 }
@@ -250,59 +252,61 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
   constexpr int LPR = D / 8;
   const int l = blockIdx.y, b = blockIdx.z, per = Hkv * LPR;
   const ikv_session s = sess[b];
-  const int k0 = blockIdx.x * group;
-  const int todo = quant_places(group, quant_rows(s, n_rows, b), k0, per);
-  const int64_t e0 = s.slot_off + k0;
-  for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
-    uint2 wk[QU], wv[QU];
-    float2 sc[QU];
-    uint8_t bk[QU], bv[QU];
-    int64_t to[QU], from[QU];
-    bool on[QU];
+  const int rows = quant_rows(s, n_rows, b);
+  for (int k0 = blockIdx.x * group; k0 < rows; k0 += gridDim.x * group) {
+    const int todo = quant_places(group, rows, k0, per);
+    const int64_t e0 = s.slot_off + k0;
+    for (int i0 = threadIdx.x; i0 < todo; i0 += QT * QU) {
+      uint2 wk[QU], wv[QU];
+      float2 sc[QU];
+      uint8_t bk[QU], bv[QU];
+      int64_t to[QU], from[QU];
+      bool on[QU];
 #pragma unroll
-    for (int u = 0; u < QU; ++u) {
-      const int i = min(i0 + u * QT, todo - 1), k = i / per, at = i - k * per;
-      const int64_t e = e0 + k;
-      const int slot = src[e];
-      on[u] = i0 + u * QT < todo && slot != dead;
-      from[u] = (int64_t(l) * num_slots + slot) * per + at;                    // 8-code pieces
-      to[u] = ((int64_t(l) * pool_slots + (dst ? int64_t(dst[e]) : e)) * per + at) * 8;
-    }
+      for (int u = 0; u < QU; ++u) {
+        const int i = min(i0 + u * QT, todo - 1), k = i / per, at = i - k * per;
+        const int64_t e = e0 + k;
+        const int slot = src[e];
+        on[u] = i0 + u * QT < todo && slot != dead;
+        from[u] = (int64_t(l) * num_slots + slot) * per + at;                    // 8-code pieces
+        to[u] = ((int64_t(l) * pool_slots + (dst ? int64_t(dst[e]) : e)) * per + at) * 8;
+      }
 #pragma unroll
-    for (int u = 0; u < QU; ++u)
-      if (on[u]) {
-        if constexpr (FOUR) {
-          wk[u].x = reinterpret_cast<const uint32_t *>(kc)[from[u]];
-          wv[u].x = reinterpret_cast<const uint32_t *>(vc)[from[u]];
-          const uint8_t *p = static_cast<const uint8_t *>(scales) + from[u] / LPR * (D / 16) + from[u] % LPR / 4;
-          bk[u] = p[0];
-          bv[u] = p[D / 32];
-        } else {
-          wk[u] = reinterpret_cast<const uint2 *>(kc)[from[u]];
-          wv[u] = reinterpret_cast<const uint2 *>(vc)[from[u]];
-          sc[u] = reinterpret_cast<const float2 *>(scales)[from[u] / LPR];
+      for (int u = 0; u < QU; ++u)
+        if (on[u]) {
+          if constexpr (FOUR) {
+            wk[u].x = reinterpret_cast<const uint32_t *>(kc)[from[u]];
+            wv[u].x = reinterpret_cast<const uint32_t *>(vc)[from[u]];
+            const uint8_t *p = static_cast<const uint8_t *>(scales) + from[u] / LPR * (D / 16) + from[u] % LPR / 4;
+            bk[u] = p[0];
+            bv[u] = p[D / 32];
+          } else {
+            wk[u] = reinterpret_cast<const uint2 *>(kc)[from[u]];
+            wv[u] = reinterpret_cast<const uint2 *>(vc)[from[u]];
+            sc[u] = reinterpret_cast<const float2 *>(scales)[from[u] / LPR];
+          }
         }
-      }
 #pragma unroll
-    for (int u = 0; u < QU; ++u)
-      if (on[u] && FOUR) {
-        put8_e2m1(kpool + to[u], wk[u].x, bk[u]);
-        put8_e2m1(vpool + to[u], wv[u].x, bv[u]);
-      } else if (on[u]) {
-        put8(kpool + to[u], wk[u], sc[u].x, code);
-        put8(vpool + to[u], wv[u], sc[u].y, code);
-      }
+      for (int u = 0; u < QU; ++u)
+        if (on[u] && FOUR) {
+          put8_e2m1(kpool + to[u], wk[u].x, bk[u]);
+          put8_e2m1(vpool + to[u], wv[u].x, bv[u]);
+        } else if (on[u]) {
+          put8(kpool + to[u], wk[u], sc[u].x, code);
+          put8(vpool + to[u], wv[u], sc[u].y, code);
+        }
+    }
   }
 }
 
 static int quant_group(const ikv_quant_pool &c) { return quant_group(c.Hkv * (c.D / 8)); }
-static dim3 quant_grid(const ikv_quant_pool &c, int B, int maxN) {
-  return dim3(unsigned(cdiv(maxN, quant_group(c))), unsigned(c.L), unsigned(B));
+static dim3 quant_grid(const ikv_quant_pool &c, int B, int maxN, int most) {
+  return dim3(unsigned(quant_groups(maxN, quant_group(c), int64_t(c.L) * B, most)), unsigned(c.L), unsigned(B));
 }
 
 hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
                               const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st) {
-  const dim3 grid = quant_grid(c, B, maxN);
+  const dim3 grid = quant_grid(c, B, maxN, src ? QUANT_GRID : QUANT_GRID_NEW);
   KTimer kt_("k_quant_store<T, D>", st);
   auto go = [&](auto tag, auto kernel) {
     using T = decltype(tag);
@@ -322,7 +326,7 @@ hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const 
 
 hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
                              const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st) {
-  const dim3 grid = quant_grid(c, B, maxN);
+  const dim3 grid = quant_grid(c, B, maxN, QUANT_GRID);
   KTimer kt_("k_quant_load<T, D>", st);
   auto go = [&](auto tag, auto kernel) {
     using T = decltype(tag);

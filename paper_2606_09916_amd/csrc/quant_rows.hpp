@@ -2,6 +2,8 @@
 // in here.
 #pragma once
 
+#include <stdint.h>
+
 #include <algorithm>
 
 namespace ikv {
@@ -13,6 +15,20 @@ constexpr int QUANT_MOST = (1 << 24) - 1;  // rows of a session in one call: a w
 // Entries of a workgroup: QU places per thread, one entry at least. `per` = Hkv D / 8 places an
 // entry, 8 channels of its K and of its V row each.
 constexpr int quant_group(int per) { return std::max(1, QT * QU / per); }
+
+// Workgroups that a launch has at most (or one a session and layer). The host knows the lists' room, N, not
+// n_rows: past these the workgroups stride over the list and end with its rows. Launching them is what
+// idle ones cost, 0.2 ns each (one row each of 64 sessions with room for 8201, 36 layers x 8 heads: 996 us
+// uncapped, 33 with 2^17); striding over full lists costs balance at the end (8189 rows in 4 bits, stored and
+// read back: 498 us uncapped, 498 with 2^17, 509 with 2^16, 522 with 2^15, 554 with 2^14). Rows that come
+// from a pool of new rows (no src) are mostly a step's few: one session's token 18.6 us with 2^17, 10.0
+// with 2^15.
+constexpr int QUANT_GRID = 1 << 17, QUANT_GRID_NEW = 1 << 15;
+
+// Workgroups of each of `units` sessions and layers, lists of up to `longest` entries.
+constexpr int quant_groups(int longest, int group, int64_t units, int most) {
+  return int(std::max<int64_t>(1, std::min<int64_t>((int64_t(longest) + group - 1) / group, most / units)));
+}
 
 // Places of the workgroup whose first entry is k0, in a list of `rows`. Past the list there are
 // none: the product comes after that, since a deficit of millions of entries times `per` would
