@@ -352,6 +352,12 @@ ikv_status attend(ikv::AttendArgs a, const ikv_session *sess, const ikv_session 
   return hip_status(ikv::launch_attend(a, plan, (hipStream_t)stream), what);
 }
 
+int64_t live_rows(const ikv_session *sess, int B) {
+  int64_t n = 0;
+  for (int b = 0; b < B; ++b) n += ikv::decode_live_bound(sess[b]);
+  return n;
+}
+
 // The checks that the store into and the load from the quantised cache share.
 ikv_status check_quant_rows(const ikv_quant_pool *c, const ikv_pool *p, const ikv_session *sess,
                             const ikv_session *sess_dev, int32_t B, const int32_t *cache_ids, const char *cache_what,
@@ -798,7 +804,7 @@ ikv_status ikv_quant_store(const ikv_quant_pool *cache, const ikv_pool *pool, co
   if (debug_mode() && (r = debug_quant_rows(sess, B, dst, cache->num_slots, "dst", cache->dead_slot, src,
                                             pool->num_slots, "src", true, n_rows, (hipStream_t)stream)))
     return r;
-  return hip_status(ikv::launch_quant_store(*cache, *pool, sess_dev, B, maxN, src, dst, n_rows, (hipStream_t)stream),
+  return hip_status(ikv::launch_quant_store(*cache, *pool, sess_dev, B, maxN, live_rows(sess, B), src, dst, n_rows, (hipStream_t)stream),
                     "ikv_quant_store");
 }
 
@@ -813,7 +819,7 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool, con
   if (debug_mode() && (r = debug_quant_rows(sess, B, src, cache->num_slots, "src", cache->dead_slot, dst,
                                             pool->num_slots, "dst", false, n_rows, (hipStream_t)stream)))
     return r;
-  return hip_status(ikv::launch_quant_load(*cache, *pool, sess_dev, B, maxN, src, dst, n_rows, (hipStream_t)stream),
+  return hip_status(ikv::launch_quant_load(*cache, *pool, sess_dev, B, maxN, live_rows(sess, B), src, dst, n_rows, (hipStream_t)stream),
                     "ikv_quant_load");
 }
 

@@ -323,9 +323,10 @@ hipError_t launch_prefill(const ikv_pool &pool, const ikv_session *sess_dev, int
                           const int32_t *hist, const int32_t *n_hist, double base, float decay, float *M,
                           void *q_out, void *out, float *kq, float *ws, int64_t kq_floats, hipStream_t st);
 
-hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+// rows: entries of all lists, as far as the host knows.
+hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN, int64_t rows,
                               const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
-hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN, int64_t rows,
                              const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const AttendPlan &p, hipStream_t st);
 hipError_t launch_attend_four(const AttendArgs &a, const AttendPlan &p, hipStream_t st);

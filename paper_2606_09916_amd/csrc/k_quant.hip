@@ -15,32 +15,41 @@
 //         rounds once.
 //   e2m1  the same over the 32 channels of 4 lanes, with 7 2^e >= a > 7 2^(e - 1), e <= 125: the
 //         conversion divides by 2^e, rounds once and holds what passes 6 there.
+#include <type_traits>
+
 #include "ikv_internal.hpp"
 #include "kv_codes.hpp"
 #include "quant_rows.hpp"
 
 namespace ikv {
 
-// A pool's rows, read or written, and the codes written pass the caches by: nothing here reads them again
-// (the store of 8189 rows in 4 bits, 36 x 8: 318 -> 252 us; the load of 9501, 48 x 4: 265 -> 248). Codes that
-// are read may be there still, from the call that wrote them: past the caches, 1021 rows took 30 us for 24.
+// PAST: a pool's rows, read or written, and the codes written pass the caches by, where there are more of
+// them than the caches would keep for the call that comes next (quant_rows.hpp). Codes that are read never do:
+// they may be there still, from the call that wrote them (so: 1021 rows read back in 30 us for 24).
 typedef uint32_t u32x2_q __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_q __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 ld_past(const void *p) {
+template <bool PAST> __device__ __forceinline__ uint4 ld_row(const void *p) {
+  if constexpr (!PAST) return *static_cast<const uint4 *>(p);
   const u32x4_q x = __builtin_nontemporal_load(static_cast<const u32x4_q *>(p));
   return make_uint4(x.x, x.y, x.z, x.w);
 }
-__device__ __forceinline__ void st_past(void *p, uint4 x) {
-  __builtin_nontemporal_store(u32x4_q{x.x, x.y, x.z, x.w}, static_cast<u32x4_q *>(p));
+template <bool PAST> __device__ __forceinline__ void st_row(void *p, uint4 x) {
+  if constexpr (PAST) __builtin_nontemporal_store(u32x4_q{x.x, x.y, x.z, x.w}, static_cast<u32x4_q *>(p));
+  else *static_cast<uint4 *>(p) = x;
 }
-__device__ __forceinline__ void st_past(void *p, uint2 x) {
-  __builtin_nontemporal_store(u32x2_q{x.x, x.y}, static_cast<u32x2_q *>(p));
+template <bool PAST> __device__ __forceinline__ void st_row(void *p, uint2 x) {
+  if constexpr (PAST) __builtin_nontemporal_store(u32x2_q{x.x, x.y}, static_cast<u32x2_q *>(p));
+  else *static_cast<uint2 *>(p) = x;
+}
+template <bool PAST> __device__ __forceinline__ void st_row(void *p, uint32_t x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, static_cast<uint32_t *>(p));
+  else *static_cast<uint32_t *>(p) = x;
 }
 
 template <typename T> struct Row8;               // 8 channels as loaded
 template <> struct Row8<uint16_t> {
   uint4 w;
-  __device__ __forceinline__ void ld(const uint16_t *p) { w = ld_past(p); }
+  template <bool PAST> __device__ __forceinline__ void ld(const uint16_t *p) { w = ld_row<PAST>(p); }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -52,9 +61,9 @@ template <> struct Row8<uint16_t> {
 };
 template <> struct Row8<float> {
   float4 a, b;
-  __device__ __forceinline__ void ld(const float *p) {
-    a = __builtin_bit_cast(float4, ld_past(p));
-    b = __builtin_bit_cast(float4, ld_past(p + 4));
+  template <bool PAST> __device__ __forceinline__ void ld(const float *p) {
+    a = __builtin_bit_cast(float4, ld_row<PAST>(p));
+    b = __builtin_bit_cast(float4, ld_row<PAST>(p + 4));
   }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
@@ -134,7 +143,7 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
 // 303 us (6.0 TB/s read and written), read back in 307 (6.0); 8189 in 4 bits 238 (6.4) and 254 (6.0).
 // Both calls, 4 bits, with one place a thread 518, two 498, four 507, eight 589.
 
-template <typename T, int D, bool FOUR>
+template <typename T, int D, bool FOUR, bool PAST>
 __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool, const T *__restrict__ vpool,
                                                     int64_t pool_slots, uint8_t *__restrict__ kc,
                                                     uint8_t *__restrict__ vc, void *__restrict__ scales,
@@ -166,8 +175,8 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
 #pragma unroll
       for (int u = 0; u < QU; ++u)
         if (at[u] >= 0) {
-          rk[u].ld(kpool + from[u]);
-          rv[u].ld(vpool + from[u]);
+          rk[u].template ld<PAST>(kpool + from[u]);
+          rv[u].template ld<PAST>(vpool + from[u]);
         }
 #pragma unroll
       for (int u = 0; u < QU; ++u) {
@@ -190,8 +199,8 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
         const int64_t row = to[u] + at[u] / LPR;
         const int piece = at[u] % LPR;
         if constexpr (FOUR) {
-          __builtin_nontemporal_store(w[0].x, reinterpret_cast<uint32_t *>(kc + row * (D / 2) + piece * 4));
-          __builtin_nontemporal_store(w[1].x, reinterpret_cast<uint32_t *>(vc + row * (D / 2) + piece * 4));
+          st_row<PAST>(kc + row * (D / 2) + piece * 4, w[0].x);
+          st_row<PAST>(vc + row * (D / 2) + piece * 4, w[1].x);
           if (piece % 4 == 0) {
             uint8_t *p = static_cast<uint8_t *>(scales) + row * (D / 16) + piece / 4;
             p[0] = byte[0];
@@ -199,8 +208,8 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
           }
           continue;
         }
-        st_past(kc + row * D + piece * 8, w[0]);
-        st_past(vc + row * D + piece * 8, w[1]);
+        st_row<PAST>(kc + row * D + piece * 8, w[0]);
+        st_row<PAST>(vc + row * D + piece * 8, w[1]);
         if (piece == 0) reinterpret_cast<float2 *>(scales)[row] = make_float2(sc[0], sc[1]);
       }
     }
@@ -208,20 +217,20 @@ __global__ void __launch_bounds__(QT) k_quant_store(const T *__restrict__ kpool,
 }
 
 // 8 codes of a word times their block's scale, exactly, to the pool's type.
-template <typename T> __device__ __forceinline__ void put8_e2m1(T *o, uint32_t w, uint8_t byte) {
+template <bool PAST, typename T> __device__ __forceinline__ void put8_e2m1(T *o, uint32_t w, uint8_t byte) {
   const float scale = __uint_as_float(uint32_t(byte) << 23);           // 255: NaN
   if constexpr (sizeof(T) == 4) {
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
     const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-    st_past(o, __builtin_bit_cast(uint4, make_float4(a[0], a[1], b[0], b[1])));
-    st_past(o + 4, __builtin_bit_cast(uint4, make_float4(c[0], c[1], d[0], d[1])));
+    st_row<PAST>(o, __builtin_bit_cast(uint4, make_float4(a[0], a[1], b[0], b[1])));
+    st_row<PAST>(o + 4, __builtin_bit_cast(uint4, make_float4(c[0], c[1], d[0], d[1])));
   } else {
-    st_past(o, e2m1_scaled8(w, scale));
+    st_row<PAST>(o, e2m1_scaled8(w, scale));
   }
 }
 
 // 8 codes times their scale, to the pool's type.
-template <typename T> __device__ __forceinline__ void put8(T *o, uint2 w, float scale, int code) {
+template <bool PAST, typename T> __device__ __forceinline__ void put8(T *o, uint2 w, float scale, int code) {
   const uint32_t u[2] = {w.x, w.y};
   float x[8];
 #pragma unroll
@@ -230,18 +239,18 @@ template <typename T> __device__ __forceinline__ void put8(T *o, uint2 w, float 
     x[i] = (code == IKV_INT8 ? float(int8_t(byte)) : __builtin_amdgcn_cvt_f32_fp8(byte, 0)) * scale;
   }
   if constexpr (sizeof(T) == 4) {
-    st_past(o, __builtin_bit_cast(uint4, make_float4(x[0], x[1], x[2], x[3])));
-    st_past(o + 4, __builtin_bit_cast(uint4, make_float4(x[4], x[5], x[6], x[7])));
+    st_row<PAST>(o, __builtin_bit_cast(uint4, make_float4(x[0], x[1], x[2], x[3])));
+    st_row<PAST>(o + 4, __builtin_bit_cast(uint4, make_float4(x[4], x[5], x[6], x[7])));
   } else {
     typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
     bf16x8 y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = __bf16(x[i]);
-    st_past(o, __builtin_bit_cast(uint4, y));
+    st_row<PAST>(o, __builtin_bit_cast(uint4, y));
   }
 }
 
-template <typename T, int D, bool FOUR>
+template <typename T, int D, bool FOUR, bool PAST>
 __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
                                                    const void *__restrict__ scales, int64_t num_slots, int Hkv,
                                                    int code, int dead, int group, T *__restrict__ kpool,
@@ -289,11 +298,11 @@ __global__ void __launch_bounds__(QT) k_quant_load(const uint8_t *__restrict__ k
 #pragma unroll
       for (int u = 0; u < QU; ++u)
         if (on[u] && FOUR) {
-          put8_e2m1(kpool + to[u], wk[u].x, bk[u]);
-          put8_e2m1(vpool + to[u], wv[u].x, bv[u]);
+          put8_e2m1<PAST>(kpool + to[u], wk[u].x, bk[u]);
+          put8_e2m1<PAST>(vpool + to[u], wv[u].x, bv[u]);
         } else if (on[u]) {
-          put8(kpool + to[u], wk[u], sc[u].x, code);
-          put8(vpool + to[u], wv[u], sc[u].y, code);
+          put8<PAST>(kpool + to[u], wk[u], sc[u].x, code);
+          put8<PAST>(vpool + to[u], wv[u], sc[u].y, code);
         }
     }
   }
@@ -304,43 +313,54 @@ static dim3 quant_grid(const ikv_quant_pool &c, int B, int maxN, int most) {
   return dim3(unsigned(quant_groups(maxN, quant_group(c), int64_t(c.L) * B, most)), unsigned(c.L), unsigned(B));
 }
 
-hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+static double quant_row_bytes(const ikv_quant_pool &c, const ikv_pool &p, int64_t rows) {
+  return double(rows) * c.L * c.Hkv * c.D * (p.kv_dtype == IKV_BF16 ? 4 : 8);
+}
+
+// of(a channel, D, PAST) with these as types.
+template <typename Of> static void quant_widths(bool bf16, bool d128, bool past, Of of) {
+  auto with = [&](auto tag, auto d) { past ? of(tag, d, std::true_type()) : of(tag, d, std::false_type()); };
+  auto wide = [&](auto tag) {
+    d128 ? with(tag, std::integral_constant<int, 128>()) : with(tag, std::integral_constant<int, 64>());
+  };
+  bf16 ? wide(uint16_t()) : wide(float());
+}
+
+hipError_t launch_quant_store(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN, int64_t rows,
                               const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st) {
   const dim3 grid = quant_grid(c, B, maxN, src ? QUANT_GRID : QUANT_GRID_NEW);
-  KTimer kt_("k_quant_store<T, D>", st);
+  const bool past = quant_row_bytes(c, p, rows) > QUANT_STORE_KEPT;
+  KTimer kt_(past ? "k_quant_store<past>" : "k_quant_store", st);
   auto go = [&](auto tag, auto kernel) {
     using T = decltype(tag);
     kernel<<<grid, QT, 0, st>>>(static_cast<const T *>(p.k_pool), static_cast<const T *>(p.v_pool), p.num_slots,
                                 static_cast<uint8_t *>(c.k_codes), static_cast<uint8_t *>(c.v_codes), c.scales,
                                 c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), sess_dev, src, dst, n_rows);
   };
-  auto of = [&](auto tag, auto eight, auto four) { c.code == IKV_E2M1 ? go(tag, four) : go(tag, eight); };
-  if (p.kv_dtype == IKV_BF16)
-    c.D == 128 ? of(uint16_t(), k_quant_store<uint16_t, 128, false>, k_quant_store<uint16_t, 128, true>)
-               : of(uint16_t(), k_quant_store<uint16_t, 64, false>, k_quant_store<uint16_t, 64, true>);
-  else
-    c.D == 128 ? of(float(), k_quant_store<float, 128, false>, k_quant_store<float, 128, true>)
-               : of(float(), k_quant_store<float, 64, false>, k_quant_store<float, 64, true>);
+  auto of = [&](auto tag, auto d, auto by) {
+    using T = decltype(tag);
+    c.code == IKV_E2M1 ? go(tag, k_quant_store<T, d.value, true, by.value>) : go(tag, k_quant_store<T, d.value, false, by.value>);
+  };
+  quant_widths(p.kv_dtype == IKV_BF16, c.D == 128, past, of);
   return hipGetLastError();
 }
 
-hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN,
+hipError_t launch_quant_load(const ikv_quant_pool &c, const ikv_pool &p, const ikv_session *sess_dev, int B, int maxN, int64_t rows,
                              const int32_t *src, const int32_t *dst, const int32_t *n_rows, hipStream_t st) {
   const dim3 grid = quant_grid(c, B, maxN, QUANT_GRID);
-  KTimer kt_("k_quant_load<T, D>", st);
+  const bool past = quant_row_bytes(c, p, rows) > QUANT_LOAD_KEPT;
+  KTimer kt_(past ? "k_quant_load<past>" : "k_quant_load", st);
   auto go = [&](auto tag, auto kernel) {
     using T = decltype(tag);
     kernel<<<grid, QT, 0, st>>>(static_cast<const uint8_t *>(c.k_codes), static_cast<const uint8_t *>(c.v_codes),
                                 c.scales, c.num_slots, c.Hkv, c.code, c.dead_slot, quant_group(c), static_cast<T *>(p.k_pool),
                                 static_cast<T *>(p.v_pool), p.num_slots, sess_dev, src, dst, n_rows);
   };
-  auto of = [&](auto tag, auto eight, auto four) { c.code == IKV_E2M1 ? go(tag, four) : go(tag, eight); };
-  if (p.kv_dtype == IKV_BF16)
-    c.D == 128 ? of(uint16_t(), k_quant_load<uint16_t, 128, false>, k_quant_load<uint16_t, 128, true>)
-               : of(uint16_t(), k_quant_load<uint16_t, 64, false>, k_quant_load<uint16_t, 64, true>);
-  else
-    c.D == 128 ? of(float(), k_quant_load<float, 128, false>, k_quant_load<float, 128, true>)
-               : of(float(), k_quant_load<float, 64, false>, k_quant_load<float, 64, true>);
+  auto of = [&](auto tag, auto d, auto by) {
+    using T = decltype(tag);
+    c.code == IKV_E2M1 ? go(tag, k_quant_load<T, d.value, true, by.value>) : go(tag, k_quant_load<T, d.value, false, by.value>);
+  };
+  quant_widths(p.kv_dtype == IKV_BF16, c.D == 128, past, of);
   return hipGetLastError();
 }
 

@@ -25,6 +25,13 @@ constexpr int quant_group(int per) { return std::max(1, QT * QU / per); }
 // with 2^15.
 constexpr int QUANT_GRID = 1 << 17, QUANT_GRID_NEW = 1 << 15;
 
+// Bytes of the pool's rows, K and V, up to which a store's rows and codes, and a load's rows, go through the
+// caches (256 MB): the decode after a store, and the one over rows read back, then find them there. Store and
+// decode, load and decode, E4M3, 36 layers x 8 heads, us through the caches / past them: 500 rows (74 MB)
+// 33 / 39, 36.5 / 41; 1021 (150) 59 / 64, 72 / 67; 1800 (265) 101 / 104, 114 / 113; 3000 (442) 173 / 168,
+// 203 / 192; 8192 (1208) 491 / 458, 593 / 522. In 4 bits 1021: 47 / 53, 65 / 62; 2300: 105 / 102, 137 / 126.
+constexpr double QUANT_STORE_KEPT = 256 << 20, QUANT_LOAD_KEPT = 128 << 20;
+
 // Workgroups of each of `units` sessions and layers, lists of up to `longest` entries.
 constexpr int quant_groups(int longest, int group, int64_t units, int most) {
   return int(std::max<int64_t>(1, std::min<int64_t>((int64_t(longest) + group - 1) / group, most / units)));

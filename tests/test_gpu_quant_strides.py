@@ -58,3 +58,30 @@ def test_long_padded_lists(dev, code, dtype, D, new_rows):
         full = torch.full_like(x, 3.0).cpu()
         full[:, to] = w.to(x.dtype)
         assert torch.equal(x.cpu(), full)
+
+
+# bytes of the pool's rows: 36 * 8 * 128 * 4 of an entry of N
+@pytest.mark.parametrize("N,store,load", [(100, "k_quant_store", "k_quant_load"), (900, "k_quant_store", "k_quant_load"),
+                                          (1021, "k_quant_store", "k_quant_load<past>"),
+                                          (2000, "k_quant_store<past>", "k_quant_load<past>")])
+@pytest.mark.parametrize("code", ["int8", "e2m1"])
+def test_rows_that_the_caches_keep(dev, code, N, store, load):
+    """Which calls write through the caches, for the one that reads next, and which past them."""
+    import torch
+    L, Hkv, D = 36, 8, 128
+    k, v = (torch.zeros(L, 9, Hkv, D, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    kc, vc, sc = empty_four(L, 9, Hkv, D, dev) if code == "e2m1" else empty_cache(code, L, 9, Hkv, D, dev)
+    pool, cache = ikv.make_pool(k, v, L, Hkv, Hkv, D, 9, 0), ikv.make_quant_pool(kc, vc, sc, L, Hkv, Hkv, D, 9, 0)
+    ids, n = torch.ones(N, dtype=torch.int32, device=dev), torch.ones(1, dtype=torch.int32, device=dev)
+    row = dict(slot_off=0, mem_off=0, qspan_off=0, qpos_off=0, N=N, pi=0, qs=N, qe=N, C=N, radix_prefix=0, R=1, nq=0)
+
+    def launched(call, **kw):
+        ikv.timing(True)
+        call(cache, pool, ikv.Sessions([{**row, **kw}], dev), ids, ids, n)
+        torch.cuda.synchronize()
+        ikv.timing(False)
+        return [name for name, _ in ikv.timing_read()]
+
+    assert launched(ikv.quant_store) == [store] and launched(ikv.quant_load) == [load]
+    # a list with room for a history of which the budget keeps a few
+    assert launched(ikv.quant_store, C=500) == ["k_quant_store"] and launched(ikv.quant_load, C=500) == ["k_quant_load"]
