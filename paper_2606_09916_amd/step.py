@@ -44,8 +44,11 @@ class RetentionStep:
         self.k_pool = k_dev if k_dev is not None else _t(batch.k_pool, device)
         self.v_pool = v_dev if v_dev is not None else _t(batch.v_pool, device)
         self.pool = ikv.make_pool(self.k_pool, self.v_pool, sh.L, sh.Hq, sh.Hkv, sh.D, batch.num_slots, dead_slot)
-        self.S0 = _t(batch.slot_maps.astype(np.int32), device)
-        self.S = self.S0.clone()
+        # the slot maps, and behind them n_freed, which reset() clears with them
+        total, B = int(batch.slot_maps.shape[0]), len(batch.sessions)
+        self._maps0 = torch.cat([_t(batch.slot_maps.astype(np.int32), device), torch.zeros(B, dtype=torch.int32, device=device)])
+        self._maps = self._maps0.clone()
+        self.S0, self.S, self.n_freed = self._maps0[:total], self._maps[:total], self._maps[total:]
         self.M0 = _t(batch.M.astype(np.float32), device)
         self.M = self.M0.clone()
         self.q_span = _t(batch.q_span, device)
@@ -59,14 +62,12 @@ class RetentionStep:
                              radix_prefix=s.radix_prefix, R=s.R, nq=len(s.query_positions())))
         self.sess = ikv.Sessions(rows, device)
         self.B = len(rows)
-        total = int(batch.slot_maps.shape[0])
         self.scores = torch.empty(total, dtype=torch.float32, device=device)
         self.keep = torch.empty(total, dtype=torch.uint8, device=device)
         self.freed = torch.empty(total, dtype=torch.int32, device=device)
         self.live = torch.empty(total, dtype=torch.int32, device=device)
         self.n_keep = torch.empty(self.B, dtype=torch.int32, device=device)
         self.tau = torch.empty(self.B, dtype=torch.float32, device=device)
-        self.n_freed = torch.empty(self.B, dtype=torch.int32, device=device)
         self.n_live = torch.empty(self.B, dtype=torch.int32, device=device)
         self.out = torch.empty_like(self.q_dec)
         self.ws = ikv.Workspace(device)
@@ -74,8 +75,9 @@ class RetentionStep:
 
     # ---------------------------------------------------------------- calls
     def reset(self):
-        """Restore the slot maps and the QueryMemory to their initial state."""
-        self.S.copy_(self.S0)
+        """Restore the slot maps and the QueryMemory to their initial state. Nothing is freed any more; what
+        ``return_freed`` pushed before stays on its stack."""
+        self._maps.copy_(self._maps0)
         self.M.copy_(self.M0)
 
     def init_dead_slot(self):
@@ -126,11 +128,14 @@ class RetentionStep:
                                 sinks=sinks, window=window)
 
     def return_freed(self, free):
-        """Push the slots that ``redirect`` freed onto a stack of free ones (``ikv.make_free_slots``)."""
+        """Push the slots that ``redirect`` freed onto a stack of free ones (``ikv.make_free_slots``), once: ``n_freed``
+        is zero before the first ``redirect`` and after this call, on the device, so that a captured step may hold
+        either call."""
         if (free.num_slots, free.dead_slot) != (self.num_slots, self.dead):
             raise ikv.IkvError(-1, "RetentionStep.return_freed",
                                f"free slots of a pool of {free.num_slots} slots (sentinel {free.dead_slot}), not of this one")
         ikv.return_slots(free, self.sess, self.freed, self.n_freed)
+        self.n_freed.zero_()
 
     def step(self, update_memory: bool = True):
         if update_memory:
