@@ -68,7 +68,7 @@ class RetentionStep:
         self.live = torch.empty(total, dtype=torch.int32, device=device)
         self.n_keep = torch.empty(self.B, dtype=torch.int32, device=device)
         self.tau = torch.empty(self.B, dtype=torch.float32, device=device)
-        self.n_live = torch.empty(self.B, dtype=torch.int32, device=device)
+        self.n_live = torch.zeros(self.B, dtype=torch.int32, device=device)
         self.out = torch.empty_like(self.q_dec)
         self.ws = ikv.Workspace(device)
         self.cache = None                        # the quantised cache, made by quantise()

@@ -1,10 +1,13 @@
-"""RetentionStep's counts of freed slots before there are any, and what reset() leaves (no GPU needed)."""
+"""RetentionStep's counts of freed and live slots before there are any, and what reset() leaves (no GPU needed)."""
+import pytest
 import torch
 
 from test_step_quant_args import step  # noqa: F401
 
 
-def test_nothing_is_freed_before_a_redirect(monkeypatch, request):
+@pytest.mark.parametrize("count", ["n_freed", "n_live"])
+def test_nothing_is_listed_before_a_redirect(monkeypatch, request, count):
+    """The lists themselves are not written yet: a decode, a store or a return must read none of them."""
     monkeypatch.setattr(torch.utils.deterministic, "fill_uninitialized_memory", True)
     torch.use_deterministic_algorithms(True)             # memory that nobody wrote holds the largest value
     try:
@@ -12,7 +15,7 @@ def test_nothing_is_freed_before_a_redirect(monkeypatch, request):
         assert torch.empty(3, dtype=torch.int32).min() > 0
     finally:
         torch.use_deterministic_algorithms(False)
-    assert st.n_freed.tolist() == [0]
+    assert getattr(st, count).tolist() == [0]
 
 
 def test_reset_restores_the_maps_and_frees_nothing(step):  # noqa: F811
