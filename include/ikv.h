@@ -587,9 +587,21 @@ typedef struct ikv_free_slots {
 
 /*
  * Push slots onto the stack: entries list[slot_off + k], k < n_list[b] (clamped to [0, N]), of
- * session after session, in order. ikv_redirect_slots' freed and n_freed, or live and n_live of
- * a request that ends. The sentinel and slots that are free already must not be listed; what
- * would not fit into num_slots entries is dropped. Only N and slot_off of the sessions are read.
+ * session after session, in order. Only N and slot_off of the sessions are read, and the entries
+ * are not looked at: each must be a slot that nobody uses any more, listed once. The sentinel,
+ * slots that are free already, slots listed twice (in one session or in two) and slots that
+ * another request still reads or that must outlive this one (a shared prefix) must not be listed:
+ * the take would hand them to new tokens, whose rows overwrite them.
+ *   freed and n_freed of ikv_redirect_slots are such a list, per session: each slot once, none of
+ *     positions below radix_prefix. Slots past it that two sessions share are in the lists of both.
+ *   live and n_live of a request that ends are not, in general: they name the slots of all its
+ *     positions, those below radix_prefix too, and an aliased slot as often as it occurs. Such a
+ *     request ends by a redirect that keeps the positions below radix_prefix and no other (so a
+ *     later position that aliases one of their slots does not free it) and the return of what that
+ *     freed; slots that its live list has and its slot map has not (taken with slot_maps NULL) are
+ *     returned from the list.
+ * What would not fit into num_slots entries is dropped. IKV_DEBUG=1 refuses the sentinel, slots
+ * that are free already and repeats; it cannot see who else uses a slot.
  */
 ikv_status ikv_return_slots(const ikv_free_slots *free_slots, const ikv_session *sess,
                             const ikv_session *sess_dev, int32_t B, const int32_t *list,

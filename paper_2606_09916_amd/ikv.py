@@ -415,7 +415,8 @@ def attend_chunk_quant(cache: QuantPool, sess: Sessions, q, live, n_live, out, w
 
 
 def return_slots(free: FreeSlots, sess: Sessions, lists, n_list, stream=None) -> None:
-    """Push the sessions' lists (n_list[b] entries from slot_off on) onto the stack of free slots, in order."""
+    """Push the sessions' lists (n_list[b] entries from slot_off on) onto the stack of free slots, in order: what a
+    redirect freed, or other slots that nobody uses any more, each once. A live list may hold others (a shared prefix)."""
     what = "ikv_return_slots"
     _lists(sess, (lists,), n_list, what, ("lists",))
     st = _place(what, sess, stream, free, lists, n_list)
