@@ -533,7 +533,9 @@ ikv_status ikv_quant_load(const ikv_quant_pool *cache, const ikv_pool *pool,
  *     for bf16 outputs two (2^-17) where the longest chunk of the call has up to 16 query rows a
  *     KV head (tokens times Hq / Hkv; 32 over the quantised cache), and one (2^-8, to nearest; their
  *     sum is of the unrounded ones) where it has more. Entries a token does not see add nothing to it, whatever their
- *     rows and scales hold.
+ *     rows and scales hold. A 4-bit value that a token sees and that stands for an infinity makes
+ *     its channel that infinity (NaN where both signs meet, and it may be NaN where its weight
+ *     is below 2^-126 of the largest); a seen infinity of a bf16 pool may give NaN.
  *   q, out: device, 16-byte aligned, packed by session (session b's rows start after those of
  *     the sessions before it), [L][Hq][n][D] each: [B][L][Hq][D] for the decode. Their type is
  *     io_dtype of the cache, or bf16 for ikv_attend_chunk, which needs a bf16 pool

@@ -196,10 +196,12 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
       }
       float kscale[2];                             // E2M1: of this lane's block of key row 16 kb + c
       uint32_t vscale[2];                          // and the bytes of its values' blocks, in the order of x.v
+      bool odd_scale = false;                      // some byte of them is 253 or more
       if constexpr (FMT == KV_E2M1) {
         uint8_t *vb = reinterpret_cast<uint8_t *>(sc[w][1]);
+        const uint32_t kw = __float_as_uint(x.s.x), vw = D == 128 ? __float_as_uint(x.s.y) : kw >> 16;
+        odd_scale = __builtin_amdgcn_ballot_w64(scales_odd(vw)) != 0;
         if (lane < FEW_BLOCK) {
-          const uint32_t kw = __float_as_uint(x.s.x), vw = D == 128 ? __float_as_uint(x.s.y) : kw >> 16;
           sc[w][0][lane] = __uint_as_float(kw);
 #pragma unroll
           for (int i = 0; i < D / 32; ++i) vb[FEW_BLOCK * i + lane] = uint8_t(vw >> (8 * i));
@@ -300,7 +302,9 @@ k_attend_few(AttendArgs a, int heads, int rows_max) {
         split_parts<PP>(pw, pf[k]);
       }
       if constexpr (FMT == KV_E2M1) {
-        if (!whole && __builtin_amdgcn_ballot_w64(scales_odd(vscale[0]) | scales_odd(vscale[1])) != 0) {
+        // (infinite ones in any block: k_attend_four.hip)
+        if (odd_scale &&
+            (!whole || __builtin_amdgcn_ballot_w64(scales_infinite(vscale[0]) | scales_infinite(vscale[1])) != 0)) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const uint32_t byte = vscale[e >> 2] >> (8 * (e & 3)) & 255u, z = e2m1_odd(x.v[e][0], byte);

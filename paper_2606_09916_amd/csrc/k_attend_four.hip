@@ -178,8 +178,14 @@ k_attend_four(AttendArgs a, int heads, int rows_max) {
           vb[h][kb] = x.s[kb][h].y >> (8 * g) & 255u;
           top = max(top, vb[h][kb]);
         }
-      if (!whole) {
-        if (__builtin_amdgcn_ballot_w64(top >= 253u) != 0) {
+      // values that are not finite are added after the loop to the rows that see them: in a block that some
+      // row does not see, and everywhere the infinite ones, whose products with the weights' second parts
+      // (zero, or of the other sign) would be NaN
+      if (__builtin_amdgcn_ballot_w64(top >= 253u) != 0) {
+        bool out = !whole;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) out |= (vb[h][0] - 253u < 2u) | (vb[h][1] - 253u < 2u);
+        if (__builtin_amdgcn_ballot_w64(out) != 0) {
 #pragma unroll
           for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -193,6 +199,8 @@ k_attend_four(AttendArgs a, int heads, int rows_max) {
               if (vb[h][kb] == 255u) vb[h][kb] = 127u;
             }
         }
+      }
+      if (!whole) {
 #pragma unroll
         for (int k = 0; k < NR; ++k)
 #pragma unroll

@@ -226,7 +226,7 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
     // of rows that do not see it into NaN: in a tile that some row does not see whole it is left
     // out and added after the loop.
     bool odd = false;
-    auto put = [&](uint16_t *dst, uint4 x, float scale, bool look) __attribute__((always_inline)) {
+    auto put = [&](uint16_t *dst, uint4 x, float scale, bool value, bool look) __attribute__((always_inline)) {
       if constexpr (FMT == KV_BF16) {
         if (look) {
           odd |= odd_low(x.x) | odd_high(x.x) | odd_low(x.y) | odd_high(x.y) | odd_low(x.z) | odd_high(x.z) |
@@ -235,7 +235,10 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
         }
         *reinterpret_cast<uint4 *>(dst) = x;
       } else if constexpr (FMT == KV_E2M1) {
-        if (look && __builtin_amdgcn_ballot_w64(!(fabsf(scale) < 0x1p126f)) != 0) {
+        // (infinite ones in any tile where the weights have several parts: k_attend_four.hip)
+        bool out = look && !(scale < 0x1p126f);
+        if constexpr (PP > 1) out |= value && scale >= 0x1p126f && scale < INFINITY;
+        if (__builtin_amdgcn_ballot_w64(out) != 0) {
 #pragma unroll
           for (int i = 0; i < PB / 4; ++i) {
             const uint32_t z = e2m1_odd((&x.x)[i], __float_as_uint(scale) >> 23);
@@ -278,8 +281,8 @@ k_attend_tile(AttendArgs a, int blocks, int nsplit, int units) {
 #pragma unroll
       for (int i = 0; i < PP_; ++i) {
         const int key = key0 + i * (NT / PPR);
-        if (takes_k) put(&ks_[par ^ 1][key * ROW + at], r.k[i], r.ks[i], false);
-        if (takes_v) put(&vs_[par][key * ROW + at], r.v[i], r.vs[i], look);
+        if (takes_k) put(&ks_[par ^ 1][key * ROW + at], r.k[i], r.ks[i], false, false);
+        if (takes_v) put(&vs_[par][key * ROW + at], r.v[i], r.vs[i], true, look);
       }
       if constexpr (FMT == KV_INT8) {
         if (tid < TILE_KEYS) {

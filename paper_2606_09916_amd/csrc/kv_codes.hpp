@@ -50,6 +50,14 @@ __device__ __forceinline__ float scale_byte(uint32_t w, int i) { return __uint_a
 // Whether some byte of a word is 253 or more.
 __device__ __forceinline__ bool scales_odd(uint32_t w) { return ((((w & 0x7f7f7f7fu) + 0x03030303u) & w) & 0x80808080u) != 0; }
 
+// Whether some byte of a word is 253 or 254.
+__device__ __forceinline__ bool scales_infinite(uint32_t w) {
+  bool x = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x |= (w >> (8 * i) & 255u) - 253u < 2u;
+  return x;
+}
+
 // Whether a scale is anything but a normal power of two: those are 0 .. 253 once the exponent is
 // rotated down, less one; a mantissa, a sign, zero and what is not finite lie above.
 __device__ __forceinline__ bool no_power(float scale) {
