@@ -61,8 +61,9 @@ inline int64_t attend_bound(const ikv_session &s, bool decode) {
   return decode ? decode_live_bound(s) : std::max<int64_t>(1, s.N);
 }
 
-// How full n > 0 workgroups leave their rounds of one per CU (or `round` in all), in percent.
-inline int64_t attend_fill(int64_t n, int64_t round = CUS) { return 100 * n / ((n + round - 1) / round * round); }
+// Rounds of one workgroup per CU (or `round` in all) that n > 0 of them take, and how full they leave those, in percent.
+inline int64_t attend_rounds(int64_t n, int64_t round = CUS) { return (n + round - 1) / round; }
+inline int64_t attend_fill(int64_t n, int64_t round = CUS) { return 100 * n / (attend_rounds(n, round) * round); }
 
 // Workgroups of the few-rows kernel: `heads` adjacent KV heads (their rows lie side by side, so
 // together the waves read long pieces) times `parts` waves that share a head's entries and join
@@ -82,10 +83,13 @@ inline int64_t attend_fill(int64_t n, int64_t round = CUS) { return 100 * n / ((
 // A split's state costs rows (D + 2) floats, written and read: lists are cut no finer than 16
 // entries a row, nor for their unevenness finer than 128 (3 tokens of 5 heads in 4 sessions of
 // 700 to 2500: one split 72, four 79, six 87).
-//  - k_attend_four (p.four) takes four waves for them and fills its round to 90%: one session of 8201,
+//  - k_attend_four (p.four) takes four waves for them and fills its rounds to 90%, or to 85% where 90% takes
+//    more rounds, or where neither can be had as far as it goes with the fewest splits: one session of 8201,
 //    pairs of heads: (4, 1, 7) 63, (4, 1, 5) 76, (4, 2, 7) 69, (2, 2, 7) 72; 48 layers x 92,300:
 //    (4, 1, 5) 837, (4, 2, 5) 854, (4, 1, 10) 869; 16 sessions of 3000: (4, 1, 2) 373, (4, 1, 1) 400,
 //    (4, 2, 1) 406; 4 tokens of 5 heads in 4 sessions of 800 to 3100, 48 x 4: (4, 1, 4) 67, (4, 1, 1) 104.
+//    28 layers x 4 heads, in 87% and next in 98% or 100% of their rounds: 4 sessions of 3000 (2, 2, 2) 42,
+//    (1, 4, 6) 56; 8 of 3000 (2, 2, 1) 76, (2, 2, 8) 93; one of 30,000 (1, 4, 4) 95, (1, 4, 9) 102.
 inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t longest, bool uneven) {
   int widest = 4;
   while (Hkv % widest) widest /= 2;
@@ -102,12 +106,17 @@ inline void attend_few_shape(AttendPlan &p, int Hkv, int64_t groups, int64_t lon
     const int64_t units = heads_all / p.heads, finest = std::max(64, 16 * p.rows),
                   most = std::min<int64_t>(DEC_MAX_SPLITS, longest / (finest * p.parts));
     p.splits = 0;
-    for (int64_t s = 1; s <= most && !p.splits; ++s)
-      if (attend_fill(units * s) >= (p.four ? 90 : longest / (s * p.parts) >= 4096 ? 95 : 70) &&
-          (!uneven || units * s >= 4 * CUS || longest / (s + 1) < 128 * p.rows))
-        p.splits = int(s);
+    int64_t best = 0, best_fill = 0;
+    for (int64_t s = 1; s <= most && !p.splits; ++s) {
+      if (uneven && units * s < 4 * CUS && longest / (s + 1) >= 128 * p.rows) continue;
+      if (p.four && best_fill >= 85 && attend_rounds(units * s) > attend_rounds(units * best)) break;
+      const int64_t fill = attend_fill(units * s);
+      if (fill >= (p.four ? 90 : longest / (s * p.parts) >= 4096 ? 95 : 70)) p.splits = int(s);
+      else if (fill > best_fill) best = s, best_fill = fill;
+    }
+    if (p.four && !p.splits && best_fill >= 85) p.splits = int(best);
     if ((p.splits && p.splits <= 8) || p.heads == 1) {
-      if (!p.splits) p.splits = int(std::max<int64_t>(1, most));
+      if (!p.splits) p.splits = int(std::max<int64_t>(1, p.four && best ? best : most));
       if (!p.four && units * p.splits > CUS && longest / p.splits >= 2048 && p.rows <= FEW_ROWS) p.parts *= 2;
       return;
     }
