@@ -140,7 +140,7 @@ __device__ __forceinline__ int quant_rows(const ikv_session &s, const int32_t *n
 // work, a thread's 8 channels of its K and of its V row. A thread takes QU places at a time,
 // all their slots loaded first, then all their rows: bound by memory, the kernels need that
 // many bytes in flight per CU. 8192 rows of 36 layers x 8 heads, D = 128, bf16, E4M3: stored in
-// 303 us (6.0 TB/s read and written), read back in 307 (6.0); 8189 in 4 bits 238 (6.4) and 254 (6.0).
+// 303 us (6.0 TB/s read and written), read back in 307 (6.0); 8189 in 4 bits 240 (6.4) and 258 (5.9).
 // Both calls, 4 bits, with one place a thread 518, two 498, four 507, eight 589.
 
 template <typename T, int D, bool FOUR, bool PAST>
